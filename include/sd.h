@@ -233,6 +233,132 @@ int sd_commit(sd_ctx *c, const int32_t *seq_ids /*dev*/, int32_t n_seq, int32_t 
 int sd_route(const float *W, const float *b, int32_t n_drafts, int32_t emb_dim, const float *prompt_emb,
              int32_t n, int32_t *draft_id, void *stream);
 
+/* ---- rotary positions ---- */
+
+/* Angles per position.  Pair i of rot_dim / 2 turns by pos * f_i radians, f_i = base^(-2i / rot_dim), scaled for contexts
+ * longer than the trained ones:
+ *   SD_ROPE_PLAIN   f_i
+ *   SD_ROPE_LINEAR  f_i / factor: every position moves closer
+ *   SD_ROPE_BANDS   by the turns r = trained_len * f_i / (2 pi) that the pair makes over the trained length: k f_i + (1 - k) f_i / factor
+ *                   with k = (r - low) / (high - low) clamped to [0, 1] (fast pairs stay, slow ones are divided by factor)
+ *   SD_ROPE_RAMP    the same mixture, k falling linearly in the pair's index between the pair that makes `high` turns (rounded
+ *                   down) and the one that makes `low` turns (rounded up)
+ * factor, low, high and trained_len are read only where a formula names them. */
+enum { SD_ROPE_PLAIN = 0, SD_ROPE_LINEAR = 1, SD_ROPE_BANDS = 2, SD_ROPE_RAMP = 3 };
+typedef struct {
+    int32_t rot_dim;      /* even, 2..512 */
+    int32_t scaling;      /* SD_ROPE_* */
+    double base;          /* > 1 */
+    double factor;        /* >= 1 */
+    double low, high;     /* 0 < low < high */
+    double trained_len;   /* >= 1 */
+} sd_rope_config;
+/* Host only (no GPU call): the rot_dim / 2 values f_i into inv_freq (host). */
+int sd_rope_freqs(const sd_rope_config *cfg, double *inv_freq);
+
+/* Model m's positions turn by these angles from the next forward on, gain multiplying cosine and sine (1 unless the
+ * scaling calls for another).  The path pairs dimension i with i + head_dim / 2 over the whole head: cfg->rot_dim must be
+ * head_dim (SD_EINVAL).  Cache rows already written keep their angles.  Synchronises. */
+int sd_model_set_rope(sd_model *m, const sd_rope_config *cfg, double gain);
+
+/* Rotary positions of rows the caller holds: for each row r and head, every pair (a, b) of the first rot_dim dimensions becomes
+ *   gain * (a cos t - b sin t, b cos t + a sin t),  t = pos[r] * inv_freq[i]
+ * and the other dimensions stay as they are.  inverse != 0 turns by -t: with the same gain that is the gradient of the forward
+ * call.  interleaved = 0 pairs dimensions (i, i + rot_dim / 2), 1 pairs (2i, 2i + 1).  The angle is formed and reduced in 64
+ * bits (positions of millions lose nothing), sine, cosine and products are 32-bit, rounded once to dtype.
+ *   x, y dev, dtype (SD_FP32 or SD_BF16), element (row, head, d) at row * *_row + head * *_head + d; queries and keys that lie
+ *   in one packed buffer can be turned by one call.  y == x with the same strides works in place; otherwise they must not
+ *   overlap.  pos dev int32[n_rows] (any order, any value); inv_freq dev fp64[rot_dim / 2]
+ *   n_rows, n_heads >= 1; head_dim 2..512; rot_dim even, 2..head_dim; strides >= head_dim, or >= 0 where there is one row or head
+ * 16-byte accesses where pointers, strides and widths allow them, element by element otherwise.  Only enqueues on `stream`. */
+int sd_rope(const void *x, int64_t x_row, int64_t x_head, void *y, int64_t y_row, int64_t y_head, int32_t dtype, int32_t n_rows,
+            int32_t n_heads, int32_t head_dim, int32_t rot_dim, const int32_t *pos, const double *inv_freq, float gain,
+            int32_t interleaved, int32_t inverse, void *stream);
+
+/* ---- caches in 8 bits ----
+ *
+ * Keys and values as 8-bit integers with a 32-bit scale for each (token, head):
+ *   scale = max(max_d |x_d| * (1 / 127), 2^-60),  code_d = the integer nearest to x_d / scale, ties to even;  it stands for code * scale
+ * so that a value is off by at most half a scale.  1 / 127 and the product with it are rounded to 32 bits, the codes are exactly
+ * the nearest integers.  A row with a NaN or an infinity gets scale NaN and codes 0.  A block of scaling is one token:
+ * with more, an outlier among rejected candidates would coarsen committed tokens for good, and what a cache holds would depend
+ * on how many candidates were tried.
+ *
+ * The caller owns the memory; the struct only names it (all pointers dev).  Sequence b holds rows off[b] .. off[b] + cap[b]
+ * of every head.  Lengths are not part of it: a call takes the number of tokens each sequence held BEFORE its new rows, so a
+ * step appends and attends with the same array, and rolling back is not advancing it. */
+typedef struct {
+    int8_t *k, *v;           /* [n_kv_heads][tokens][head_dim], 16-byte aligned */
+    float *k_scale, *v_scale; /* [n_kv_heads][tokens] */
+    int64_t tokens;          /* rows per head */
+    int32_t n_kv_heads;      /* >= 1 */
+    int32_t head_dim;        /* a multiple of 16 in 16..256 */
+    int32_t n_seq;           /* >= 1 */
+    const int64_t *off;      /* int64[n_seq], every off[b] + cap[b] <= tokens */
+    const int32_t *cap;      /* int32[n_seq] */
+    int32_t *status;         /* int32[1] or NULL: sticky bits, 1 = a row outside its sequence's capacity, 4 = a sequence id out of range */
+} sd_kv8;
+
+/* Rows of a call belong to n_seq sequences seq_ids (dev int32[n_seq], or NULL for 0..n_seq-1; distinct).  row_start NULL: `rows`
+ * rows in all, the same number of each sequence (a multiple of n_seq), in order.  row_start dev int32[n_seq + 1], ascending
+ * from 0: sequence j's rows are row_start[j] .. row_start[j+1], any number of them; `rows` (at most 2^23) is at least row_start[n_seq],
+ * and rows from there on are left alone.  Rows of a sequence id out of range are left alone.
+ *
+ * sd_kv8_append: row i of sequence b becomes its token len[b] + i (len dev int32, indexed by sequence id).  A row whose token
+ * lies outside [0, cap[b]) is not written.
+ *   k, v dev, dtype SD_FP32 or SD_BF16, element (row, head, d) at row * *_row + head * *_head + d
+ * sd_kv8_read: the reverse: row i of sequence b receives token start[b] + i, as code * scale rounded once to dtype; a row whose
+ * token lies outside [0, cap[b]) is left alone.  k or v may be NULL (not wanted).
+ * Both only enqueue one kernel on `stream`. */
+int sd_kv8_append(const sd_kv8 *c, const int32_t *seq_ids, int32_t n_seq, const int32_t *len, const int32_t *row_start,
+                  int32_t rows, int32_t dtype, const void *k, int64_t k_row, int64_t k_head, const void *v, int64_t v_row,
+                  int64_t v_head, void *stream);
+int sd_kv8_read(const sd_kv8 *c, const int32_t *seq_ids, int32_t n_seq, const int32_t *start, const int32_t *row_start,
+                int32_t rows, int32_t dtype, void *k, int64_t k_row, int64_t k_head, void *v, int64_t v_row, int64_t v_head,
+                void *stream);
+
+/* Attention over such a cache: for each row and head, softmax over the tokens it sees of scale * (q . k), times v.
+ *   causal != 0: the rows have been appended; row i of sequence b sits at token p = len[b] + i and sees tokens 0..p.  window > 0
+ *     hides what lies window or more tokens back, except the first `sinks` tokens (0: the whole context; sinks is then 0 too).
+ *   causal == 0: every row sees the len[b] tokens of its sequence (window 0).
+ * A row that sees nothing gets zeros (and a log-sum-exp of -infinity).  Tokens a row does not see leave no trace in it,
+ * whatever their memory holds.  Query head h reads cache head h / (n_heads / n_kv_heads).
+ * Scores, running maxima, sums and outputs are 32-bit; queries and probabilities enter the matrix cores as 16-bit terms -
+ * two each for SD_FP32 rows (22 bits), one for SD_BF16 rows (bf16 queries exactly, probabilities to 11 bits). */
+typedef struct {
+    const int32_t *seq_ids;   /* as above */
+    const int32_t *len;
+    const int32_t *row_start;
+    int32_t n_seq, rows;
+    int32_t max_rows;         /* most rows of one sequence, and ... */
+    int32_t max_len;          /* ... largest len: they choose the kernels and size launches, never decide results (both >= 0) */
+    int32_t n_heads;          /* a multiple of n_kv_heads */
+    int32_t dtype;            /* of q and out: SD_FP32 or SD_BF16 */
+    const void *q;            /* element (row, head, d) at row * q_row + head * q_head + d */
+    int64_t q_row, q_head;
+    void *out;
+    int64_t o_row, o_head;
+    float *lse;               /* [rows][n_heads] natural logarithm of the sum of exponentials of the scaled scores, or NULL */
+    float scale;              /* finite */
+    int32_t causal, window, sinks;
+    void *workspace;          /* sd_kv8_attend_workspace bytes of any contents, 16-byte aligned, this call's alone until its kernels have
+                                 run; NULL: one block per (sequence, head) walks the whole context */
+    int64_t workspace_bytes;
+} sd_kv8_attn;
+/* Only enqueues kernels on `stream`; may be captured into a graph. */
+int sd_kv8_attend(const sd_kv8 *c, const sd_kv8_attn *a, void *stream);
+/* Host-only: bytes of workspace the call would use (0: none), or SD_EINVAL (negative).  Reads no device memory. */
+int64_t sd_kv8_attend_workspace(const sd_kv8 *c, const sd_kv8_attn *a);
+
+/* sd_ctx_attach with model m's cache in 8 bits (half the memory and half the bytes attention reads): prefill, draft, verify and commit
+ * of m on this context then quantise rows as they are written and attend over the codes.  window > 0: m sees the last `window`
+ * tokens and the first `sinks` ones only (a draft that reads a bounded part of a long context).  SD_EINVAL if m is
+ * attached already in another form.  sd_ctx_set_kv quantises what it is given.  Synchronises. */
+int sd_ctx_attach_kv8(sd_ctx *c, sd_model *m, int32_t window, int32_t sinks);
+/* The reverse of sd_ctx_set_kv: the first len cache rows of one layer and sequence as k, v [len][n_heads][head_dim] in the model's
+ * dtype, in HOST or DEVICE memory; of a cache in 8 bits the values that the codes stand for.  Synchronises. */
+int sd_ctx_get_kv(sd_ctx *c, sd_model *m, int32_t layer, int32_t seq, void *k, void *v, int32_t len);
+
 /* ---- prompt classifier (Sections 2.4, 3.3.3): the second routing backend ----
  *
  * The classifier the paper describes: an embedding, one selective state-space ("Mamba")

@@ -27,7 +27,9 @@ EXPORTS = ["sd_load_model", "sd_free_model", "sd_ctx_create", "sd_ctx_free", "sd
            "sd_classifier_create", "sd_classifier_destroy", "sd_route_classifier", "sd_route_classifier_ws",
            "sd_classifier_workspace", "sd_accept",
            "sd_accept_static", "sd_debug_stream_read", "sd_debug_gemm_plan", "sd_debug_gemm_splits",
-           "sd_policy_set", "sd_policy_choose", "sd_policy_read"]
+           "sd_policy_set", "sd_policy_choose", "sd_policy_read",
+           "sd_rope_freqs", "sd_model_set_rope", "sd_rope", "sd_kv8_append", "sd_kv8_read", "sd_kv8_attend",
+           "sd_kv8_attend_workspace", "sd_ctx_attach_kv8", "sd_ctx_get_kv"]
 
 
 class SdError(RuntimeError):
@@ -62,6 +64,29 @@ class _ClsShape(C.Structure):
 
 class _ClsWeights(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in CLASSIFIER_WEIGHTS]
+
+
+ROPE_SCALINGS = {"plain": 0, "linear": 1, "bands": 2, "ramp": 3}
+
+
+class _RopeConfig(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("scaling", C.c_int32), ("base", C.c_double), ("factor", C.c_double),
+                ("low", C.c_double), ("high", C.c_double), ("trained_len", C.c_double)]
+
+
+class _Kv8(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("tokens", C.c_int64), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("n_seq", C.c_int32),
+                ("off", C.c_void_p), ("cap", C.c_void_p), ("status", C.c_void_p)]
+
+
+class _Kv8Attn(C.Structure):
+    _fields_ = [("seq_ids", C.c_void_p), ("len", C.c_void_p), ("row_start", C.c_void_p), ("n_seq", C.c_int32),
+                ("rows", C.c_int32), ("max_rows", C.c_int32), ("max_len", C.c_int32), ("n_heads", C.c_int32),
+                ("dtype", C.c_int32), ("q", C.c_void_p), ("q_row", C.c_int64), ("q_head", C.c_int64),
+                ("out", C.c_void_p), ("o_row", C.c_int64), ("o_head", C.c_int64), ("lse", C.c_void_p),
+                ("scale", C.c_float), ("causal", C.c_int32), ("window", C.c_int32), ("sinks", C.c_int32),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
 
 
 def lib():
@@ -113,6 +138,17 @@ def lib():
         L.sd_route_classifier_ws.argtypes = [vp, vp, vp, i32, i32, vp, vp, vp, vp]
         L.sd_classifier_workspace.argtypes = [vp, i32, i32]
         L.sd_classifier_workspace.restype = C.c_int64
+        i64 = C.c_int64
+        L.sd_rope_freqs.argtypes = [C.POINTER(_RopeConfig), vp]
+        L.sd_model_set_rope.argtypes = [vp, C.POINTER(_RopeConfig), C.c_double]
+        L.sd_rope.argtypes = [vp, i64, i64, vp, i64, i64, i32, i32, i32, i32, i32, vp, vp, C.c_float, i32, i32, vp]
+        L.sd_kv8_append.argtypes = [C.POINTER(_Kv8), vp, i32, vp, vp, i32, i32, vp, i64, i64, vp, i64, i64, vp]
+        L.sd_kv8_read.argtypes = L.sd_kv8_append.argtypes
+        L.sd_kv8_attend.argtypes = [C.POINTER(_Kv8), C.POINTER(_Kv8Attn), vp]
+        L.sd_kv8_attend_workspace.argtypes = [C.POINTER(_Kv8), C.POINTER(_Kv8Attn)]
+        L.sd_kv8_attend_workspace.restype = i64
+        L.sd_ctx_attach_kv8.argtypes = [vp, vp, i32, i32]
+        L.sd_ctx_get_kv.argtypes = [vp, vp, i32, i32, vp, vp, i32]
         L.sd_eq1_speedup.argtypes = [C.c_double, i32, C.c_double]
         L.sd_eq1_speedup.restype = C.c_double
         L.sd_choose_gamma.argtypes = [C.c_double, C.c_double, i32, C.POINTER(C.c_double)]
@@ -214,6 +250,13 @@ class Model:
         with torch.cuda.device(self.device):
             _check(lib().sd_model_set_lora(self.h, C.byref(w)))
 
+    def set_rope(self, scaling: str = "plain", base: float = 10000.0, factor: float = 1.0, low: float = 1.0, high: float = 4.0,
+                 trained_len: float = 8192.0, gain: float = 1.0) -> None:
+        """sd_model_set_rope: the angles this model's positions turn by from the next forward on."""
+        c = _RopeConfig(self.shape.head_dim, ROPE_SCALINGS[scaling], base, factor, low, high, trained_len)
+        with torch.cuda.device(self.device):
+            _check(lib().sd_model_set_rope(self.h, C.byref(c), gain))
+
     def close(self):
         if getattr(self, "h", None):
             lib().sd_free_model(self.h)
@@ -272,6 +315,11 @@ class Context:
 
     def attach(self, m: Model) -> None:
         _check(lib().sd_ctx_attach(self.h, m.h))
+        self._models.append(m)
+
+    def attach_kv8(self, m: Model, window: int = 0, sinks: int = 0) -> None:
+        """sd_ctx_attach_kv8: attach with the cache in 8 bits; window > 0: m sees the last `window` tokens and the first `sinks`."""
+        _check(lib().sd_ctx_attach_kv8(self.h, m.h, window, sinks))
         self._models.append(m)
 
     def set_tokens(self, seqs: Sequence[Sequence[int]], seq_ids: Optional[Sequence[int]] = None) -> None:
@@ -336,6 +384,13 @@ class Context:
         k, v = np.ascontiguousarray(k), np.ascontiguousarray(v)
         _check(lib().sd_ctx_set_kv(self.h, m.h, layer, seq, k.ctypes.data_as(C.c_void_p),
                                    v.ctypes.data_as(C.c_void_p), k.shape[0]))
+
+    def get_kv(self, m: Model, layer: int, seq: int, length: int):
+        """sd_ctx_get_kv -> (k, v), numpy [length][n_heads][head_dim]: fp32, or bf16 bit patterns (uint16) of a bf16 model."""
+        k, v = (np.empty((length, m.shape.n_heads, m.shape.head_dim), np.uint16 if m.shape.dtype == SD_BF16 else np.float32)
+                for _ in range(2))
+        _check(lib().sd_ctx_get_kv(self.h, m.h, layer, seq, k.ctypes.data_as(C.c_void_p), v.ctypes.data_as(C.c_void_p), length))
+        return k, v
 
 
 def gemm_plan(mode: int, m: int, n: int, k: int, n_per_seg: Optional[int] = None):
@@ -405,6 +460,155 @@ def sd_commit(ctx: Context, seq_ids: Optional[torch.Tensor], n_seq: int, gamma: 
               n_accepted: torch.Tensor, next_token: torch.Tensor) -> None:
     _check(lib().sd_commit(ctx.h, _dp(seq_ids), n_seq, gamma, _dp(cand), _dp(n_accepted), _dp(next_token),
                            _stream()))
+
+
+# ---------------------------------------------------------------- rotary positions and 8-bit caches
+_DTYPES = {torch.float32: SD_FP32, torch.bfloat16: SD_BF16}
+
+
+def rope_freqs(rot_dim: int, scaling: str = "plain", base: float = 10000.0, factor: float = 1.0, low: float = 1.0,
+               high: float = 4.0, trained_len: float = 8192.0) -> np.ndarray:
+    """sd_rope_freqs (host only): the angle per position of each of the rot_dim / 2 pairs, float64."""
+    out = np.empty(max(rot_dim, 0) // 2, np.float64)
+    c = _RopeConfig(rot_dim, ROPE_SCALINGS[scaling], base, factor, low, high, trained_len)
+    _check(lib().sd_rope_freqs(C.byref(c), out.ctypes.data))
+    return out
+
+
+def _rows3(t: torch.Tensor, name: str):
+    """(pointer, row stride, head stride) of a [rows][heads][dim] tensor whose dimensions are adjacent."""
+    if not t.is_cuda or t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] > 1):
+        raise ValueError(f"{name}: a GPU tensor [rows][heads][dim] with adjacent dimensions is wanted")
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def _plain(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, n: int, like: torch.Tensor):
+    """Pointer of a contiguous tensor of at least n elements on like's device (None -> NULL)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.numel() < n or not t.is_contiguous() or t.device != like.device:
+        raise ValueError(f"{name}: a contiguous {dtype} tensor of at least {n} elements on {like.device} is wanted")
+    return t.data_ptr()
+
+
+def _call_on(t: torch.Tensor, fn, *args) -> None:
+    """fn(*args, current stream of t's device) with that device current."""
+    dev = t.get_device()
+    if dev == torch.cuda.current_device():
+        rc = fn(*args, torch.cuda.current_stream().cuda_stream)
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(*args, torch.cuda.current_stream().cuda_stream)
+    if rc != SD_OK:
+        _check(rc)
+
+
+def sd_rope(x: torch.Tensor, pos: torch.Tensor, inv_freq: torch.Tensor, out: Optional[torch.Tensor] = None,
+            interleaved: bool = False, inverse: bool = False, gain: float = 1.0) -> torch.Tensor:
+    """sd_rope: x [rows][heads][dim] (fp32 or bf16, any row and head strides), pos int32 [rows], inv_freq float64 [rot_dim / 2] (all
+    on the GPU).  out: where the result goes (x itself: in place); a new contiguous tensor if None."""
+    if x.dtype not in _DTYPES:
+        raise ValueError("x: float32 or bfloat16 is wanted")
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    if out.shape != x.shape or out.dtype != x.dtype or out.device != x.device:
+        raise ValueError("out: a tensor like x is wanted")
+    rows, heads, dim = x.shape
+    _call_on(x, lib().sd_rope, *_rows3(x, "x"), *_rows3(out, "out"), _DTYPES[x.dtype], rows, heads, dim, 2 * inv_freq.numel(),
+             _plain(pos, "pos", torch.int32, rows, x), _plain(inv_freq, "inv_freq", torch.float64, 1, x), gain, int(interleaved),
+             int(inverse))
+    return out
+
+
+class Kv8Cache:
+    """sd_kv8: names the tensors of an 8-bit cache, which the caller owns: codes int8 [kv_heads][tokens][dim], scales float32
+    [kv_heads][tokens], off int64 [n_seq], cap int32 [n_seq], status int32 [1] or None (all contiguous, on one GPU)."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, off: torch.Tensor,
+                 cap: torch.Tensor, status: Optional[torch.Tensor] = None):
+        if not k.is_cuda or k.dim() != 3:
+            raise ValueError("k: a GPU tensor [kv_heads][tokens][dim] is wanted")
+        heads, tokens, dim = k.shape
+        n, n_seq = heads * tokens, cap.numel()
+        self.k, self.n_seq, self.kv_heads, self.head_dim = k, n_seq, heads, dim
+        self._keep = (v, k_scale, v_scale, off, cap, status)
+        self.c = _Kv8(_plain(k, "k", torch.int8, n * dim, k), _plain(v, "v", torch.int8, n * dim, k),
+                      _plain(k_scale, "k_scale", torch.float32, n, k), _plain(v_scale, "v_scale", torch.float32, n, k), tokens,
+                      heads, dim, n_seq, _plain(off, "off", torch.int64, n_seq, k), _plain(cap, "cap", torch.int32, n_seq, k),
+                      _plain(status, "status", torch.int32, 1, k))
+
+    @classmethod
+    def empty(cls, caps: Sequence[int], kv_heads: int, head_dim: int, device="cuda") -> "Kv8Cache":
+        """A cache of zeros with room for caps[b] tokens of sequence b."""
+        caps = [int(x) for x in caps]
+        n = sum(caps)
+        z = lambda *s, dtype=torch.int8: torch.zeros(*s, dtype=dtype, device=device)
+        off = torch.tensor(np.concatenate([[0], np.cumsum(caps)[:-1]]), dtype=torch.int64, device=device)
+        return cls(z(kv_heads, n, head_dim), z(kv_heads, n, head_dim), z(kv_heads, n, dtype=torch.float32),
+                   z(kv_heads, n, dtype=torch.float32), off, torch.tensor(caps, dtype=torch.int32, device=device),
+                   z(1, dtype=torch.int32))
+
+    @property
+    def status(self) -> Optional[torch.Tensor]:
+        return self._keep[5]
+
+    def _rows(self, length: torch.Tensor, seq_ids: Optional[torch.Tensor], row_start: Optional[torch.Tensor]):
+        n = self.n_seq if seq_ids is None else seq_ids.numel()
+        return (_plain(seq_ids, "seq_ids", torch.int32, 1, self.k), n, _plain(length, "length", torch.int32, self.n_seq, self.k),
+                _plain(row_start, "row_start", torch.int32, n + 1, self.k))
+
+
+def _kv8_move(fn, cache: Kv8Cache, length, k, v, seq_ids, row_start) -> None:
+    one = k if k is not None else v
+    if one is None or one.dtype not in _DTYPES:
+        raise ValueError("k, v: float32 or bfloat16 is wanted")
+    for t in (k, v):
+        if t is not None and (t.dtype != one.dtype or t.shape[0] != one.shape[0] or t.device != cache.k.device or
+                              tuple(t.shape[1:]) != (cache.kv_heads, cache.head_dim)):
+            raise ValueError("k, v: tensors [rows][kv_heads][dim] of one type on the cache's device are wanted")
+    none = (None, 0, 0)
+    _call_on(cache.k, fn, C.byref(cache.c), *cache._rows(length, seq_ids, row_start), one.shape[0], _DTYPES[one.dtype],
+             *(none if k is None else _rows3(k, "k")), *(none if v is None else _rows3(v, "v")))
+
+
+def sd_kv8_append(cache: Kv8Cache, length: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seq_ids: Optional[torch.Tensor] = None,
+                  row_start: Optional[torch.Tensor] = None) -> None:
+    """sd_kv8_append: rows k, v [rows][kv_heads][dim] become the tokens from length[b] on of their sequences."""
+    _kv8_move(lib().sd_kv8_append, cache, length, k, v, seq_ids, row_start)
+
+
+def sd_kv8_read(cache: Kv8Cache, start: torch.Tensor, k: Optional[torch.Tensor], v: Optional[torch.Tensor],
+                seq_ids: Optional[torch.Tensor] = None, row_start: Optional[torch.Tensor] = None) -> None:
+    """sd_kv8_read: the tokens from start[b] on into k, v [rows][kv_heads][dim]."""
+    _kv8_move(lib().sd_kv8_read, cache, start, k, v, seq_ids, row_start)
+
+
+def sd_kv8_attend(cache: Kv8Cache, length: torch.Tensor, q: torch.Tensor, out: torch.Tensor, scale: float,
+                  seq_ids: Optional[torch.Tensor] = None, row_start: Optional[torch.Tensor] = None, max_rows: int = 0,
+                  max_len: int = 0, causal: bool = True, window: int = 0, sinks: int = 0,
+                  lse: Optional[torch.Tensor] = None) -> None:
+    """sd_kv8_attend: q, out [rows][heads][dim]; lse float32 [rows][heads].  max_len: the largest length (and, with row_start, max_rows
+    the most rows of one sequence), as far as the caller knows them: they size launches, not results.  The workspace is the
+    caching allocator's, in order with the current stream; without memory for it the call runs without one."""
+    if q.dtype not in _DTYPES or out.dtype != q.dtype or out.shape != q.shape or q.device != cache.k.device or out.device != q.device:
+        raise ValueError("q, out: float32 or bfloat16 tensors of one shape on the cache's device are wanted")
+    if q.dim() != 3 or q.shape[2] != cache.head_dim:
+        raise ValueError("q: a tensor [rows][heads][dim] with the cache's dim is wanted")
+    rows, heads, _ = q.shape
+    ids, n, lens, starts = cache._rows(length, seq_ids, row_start)
+    a = _Kv8Attn(ids, lens, starts, n, rows, max_rows, max_len, heads, _DTYPES[q.dtype], *_rows3(q, "q"), *_rows3(out, "out"),
+                 _plain(lse, "lse", torch.float32, rows * heads, q), scale, int(causal), window, sinks, None, 0)
+    need = lib().sd_kv8_attend_workspace(C.byref(cache.c), C.byref(a))
+    if need < 0:
+        _check(need)
+    ws = None
+    if need:
+        try:
+            ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+            a.workspace, a.workspace_bytes = ws.data_ptr(), need
+        except torch.OutOfMemoryError:
+            pass
+    _call_on(cache.k, lib().sd_kv8_attend, C.byref(cache.c), C.byref(a))
 
 
 def eq1_speedup(alpha: float, gamma: int, c: float) -> float:

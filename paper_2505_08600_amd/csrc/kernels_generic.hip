@@ -2895,6 +2895,32 @@ hipError_t launch_set_kv(hipStream_t s, int dtype, const void *k_rows, const voi
     return hipGetLastError();
 }
 
+template <typename T>
+__global__ void get_kv_kernel(T *k_rows, T *v_rows, int len, int H, int hd, int64_t seq_off, int64_t total_cap, const T *Kl, const T *Vtl)
+{
+    size_t n = (size_t)len * H * hd;
+    for (size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (size_t)gridDim.x * blockDim.x) {
+        int d = i % hd;
+        int h = (i / hd) % H;
+        int t = i / ((size_t)hd * H);
+        k_rows[i] = Kl[(size_t)h * total_cap * hd + kt_offset(hd, seq_off + t, d)];
+        v_rows[i] = Vtl[(size_t)h * hd * total_cap + vt_offset(hd, seq_off + t, d)];
+    }
+}
+
+hipError_t launch_get_kv(hipStream_t s, int dtype, void *k_rows, void *v_rows, int len, int H, int hd, int64_t seq_off, int64_t total_cap,
+                         const void *Kl, const void *Vtl)
+{
+    const int blocks = (int)std::min<size_t>(65535, ((size_t)len * H * hd + 255) / 256);
+    if (dtype == SD_BF16)
+        hipLaunchKernelGGL(get_kv_kernel<bf16_t>, dim3(blocks), dim3(256), 0, s, (bf16_t *)k_rows, (bf16_t *)v_rows, len, H, hd, seq_off, total_cap,
+                           (const bf16_t *)Kl, (const bf16_t *)Vtl);
+    else
+        hipLaunchKernelGGL(get_kv_kernel<float>, dim3(blocks), dim3(256), 0, s, (float *)k_rows, (float *)v_rows, len, H, hd, seq_off, total_cap,
+                           (const float *)Kl, (const float *)Vtl);
+    return hipGetLastError();
+}
+
 // ---------------------------------------------------------------- measurement helper: a plain streaming read
 // Reads `n_vec` 16-byte vectors once and folds them into one word (written only if it hits a magic value, so that
 // the loads cannot be dropped): what the memory system gives a kernel that does nothing but read, the practical

@@ -1,0 +1,404 @@
+// An 8-bit cache of keys and values: quantising rows as they are written, reading them back, and the calls of the C ABI.
+//
+// A vector is one row of one head, K or V: scale = max|x| * (1 / 127), at least 2^-60, code = nearest integer to x / scale.
+// Bound of both kernels: memory.  D / 8 lanes hold a vector, 8 elements each: a 16-byte load (two for fp32), a maximum over the
+// lanes, an 8-byte store.  A block serves one row of the call, so that finding the row's sequence and place costs a block one
+// chain of small loads and not one per vector.
+#include <cmath>
+
+#include <algorithm>
+
+#include "kv8.h"
+
+template <typename T, bool WIDE>
+__device__ __forceinline__ void load8(const T *p, float x[8])
+{
+    if constexpr (WIDE && sizeof(T) == 2) {
+        const uint4 w = *(const uint4 *)p;
+        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int e = 0; e < 4; e++) x[2 * e] = __uint_as_float(u[e] << 16), x[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
+    } else if constexpr (WIDE) {
+        const float4 a = *(const float4 *)p, b = *(const float4 *)(p + 4);
+        x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; e++) x[e] = to_float(p[e]);
+    }
+}
+
+template <typename T, bool WIDE>
+__device__ __forceinline__ void store8(T *p, const float x[8])
+{
+    if constexpr (WIDE && sizeof(T) == 2) {
+        *(uint4 *)p = make_uint4(bf16x2_bits_rne(x[0], x[1]), bf16x2_bits_rne(x[2], x[3]), bf16x2_bits_rne(x[4], x[5]), bf16x2_bits_rne(x[6], x[7]));
+    } else if constexpr (WIDE) {
+        *(float4 *)p = make_float4(x[0], x[1], x[2], x[3]);
+        *(float4 *)(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; e++) p[e] = from_float<T>(x[e]);
+    }
+}
+
+// Largest magnitude of 8 elements as bits (a NaN's are above infinity's, which are above every finite value's) ...
+__device__ __forceinline__ uint32_t amax_bits8(const float x[8])
+{
+    uint32_t m = 0;
+#pragma unroll
+    for (int e = 0; e < 8; e++) m = max(m, __float_as_uint(x[e]) & 0x7fffffffu);
+    return m;
+}
+// ... over the `width` (a power of two) lanes of a vector ...
+__device__ __forceinline__ uint32_t amax_lanes(uint32_t m, int width)
+{
+    for (int o = 1; o < width; o <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
+    return m;
+}
+// ... and the scale it gives: NaN where the vector holds a NaN or an infinity.
+__device__ __forceinline__ float kv8_scale(uint32_t amax)
+{
+    return amax >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : fmaxf(__uint_as_float(amax) * (1.0f / 127.0f), KV8_SCALE_MIN);
+}
+
+// The integer nearest to x / s, ties to even.  x * (1 / s) is off by a few parts in 2^24, so its rounding can end on the wrong
+// side of a half; e = x - q s is exact (a multiple of the coarser of the two last places, and no larger than s), so comparing it
+// with s / 2 settles the case.
+__device__ __forceinline__ int quantise(float x, float s, float inv)
+{
+    const float q = rintf(x * inv), e = fmaf(-q, s, x), half = 0.5f * s;
+    int c = (int)q;
+    const bool over = fabsf(e) > half || (fabsf(e) == half && (c & 1));
+    return over ? c + (e > 0.f ? 1 : -1) : c;
+}
+__device__ __forceinline__ uint32_t quantise4(const float x[4], float s, float inv)
+{
+    uint32_t u = 0;
+#pragma unroll
+    for (int e = 0; e < 4; e++) u |= ((uint32_t)quantise(x[e], s, inv) & 255u) << (8 * e);
+    return u;
+}
+// codes of four bytes, as values
+__device__ __forceinline__ void dequantise4(uint32_t u, float s, float x[4])
+{
+#pragma unroll
+    for (int e = 0; e < 4; e++) x[e] = (float)((int32_t)(u << (24 - 8 * e)) >> 24) * s;
+}
+
+// Place of row r: its cache row in every head, or -1 (none: not a row of the call, or outside its sequence).
+__device__ __forceinline__ int64_t row_place(const Kv8View &c, const Kv8Rows &rw, int r, bool flag)
+{
+    const int j = kv8_owner(rw, r);
+    if (j < 0 || j >= rw.n) return -1;
+    const Kv8Seq s = kv8_seq(c, rw, j);
+    if (s.b < 0) {
+        if (flag && c.status) atomicOr(c.status, 4);
+        return -1;
+    }
+    const int64_t t = (int64_t)s.len + (r - s.row0);
+    if (t < 0 || t >= c.cap[s.b]) {
+        if (flag && c.status) atomicOr(c.status, 1);
+        return -1;
+    }
+    return c.off[s.b] + t;
+}
+
+template <typename T, bool WIDE>
+__global__ __launch_bounds__(256) void kv8_append_kernel(Kv8View c, Kv8Rows rw, int lanes, const T *__restrict__ k, int64_t k_row, int64_t k_head,
+                                                         const T *__restrict__ v, int64_t v_row, int64_t v_head)
+{
+    const int r = blockIdx.x;
+    const int64_t at = row_place(c, rw, r, threadIdx.x == 0 && blockIdx.y == 0);
+    if (at < 0) return;
+    const int per_block = 256 / lanes, l = threadIdx.x & (lanes - 1);
+    const bool mine = l * 8 < c.hd;
+    for (int u = blockIdx.y * per_block; u < 2 * c.kv_heads; u += gridDim.y * per_block) { // (the same count for every lane: shuffles)
+        const int w = min(u + (int)threadIdx.x / lanes, 2 * c.kv_heads - 1);
+        const int h = w >> 1;
+        const T *src = w & 1 ? v + r * v_row + h * v_head : k + r * k_row + h * k_head;
+        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (mine) load8<T, WIDE>(src + 8 * l, x);
+        const float s = kv8_scale(amax_lanes(amax_bits8(x), lanes)), inv = 1.0f / s;
+        const bool fine = s == s;
+        if (u + (int)threadIdx.x / lanes >= 2 * c.kv_heads || !mine) continue;
+        const int64_t row = (int64_t)h * c.tokens + at;
+        const uint2 codes = fine ? make_uint2(quantise4(x, s, inv), quantise4(x + 4, s, inv)) : make_uint2(0, 0);
+        *(uint2 *)((w & 1 ? c.v : c.k) + row * c.hd + 8 * l) = codes;
+        if (l == 0) (w & 1 ? c.vs : c.ks)[row] = s;
+    }
+}
+
+template <typename T, bool WIDE>
+__global__ __launch_bounds__(256) void kv8_read_kernel(Kv8View c, Kv8Rows rw, int lanes, T *__restrict__ k, int64_t k_row, int64_t k_head,
+                                                       T *__restrict__ v, int64_t v_row, int64_t v_head)
+{
+    const int r = blockIdx.x;
+    const int64_t at = row_place(c, rw, r, threadIdx.x == 0 && blockIdx.y == 0);
+    if (at < 0) return;
+    const int per_block = 256 / lanes, l = threadIdx.x & (lanes - 1);
+    if (l * 8 >= c.hd) return;
+    for (int w = blockIdx.y * per_block + threadIdx.x / lanes; w < 2 * c.kv_heads; w += gridDim.y * per_block) {
+        const int h = w >> 1;
+        T *dst = w & 1 ? v : k;
+        if (!dst) continue;
+        dst += w & 1 ? r * v_row + h * v_head : r * k_row + h * k_head;
+        const int64_t row = (int64_t)h * c.tokens + at;
+        const uint2 u = *(const uint2 *)((w & 1 ? c.v : c.k) + row * c.hd + 8 * l);
+        const float s = (w & 1 ? c.vs : c.ks)[row];
+        float x[8];
+        dequantise4(u.x, s, x);
+        dequantise4(u.y, s, x + 4);
+        store8<T, WIDE>(dst + 8 * l, x);
+    }
+}
+
+// lanes of a vector: the power of two that holds head_dim / 8
+static int vector_lanes(int hd)
+{
+    int l = 2;
+    while (l * 8 < hd) l *= 2;
+    return l;
+}
+static bool wide_rows(int esz, const void *p, int64_t row, int64_t head)
+{
+    return ((uintptr_t)p % 16) == 0 && row * esz % 16 == 0 && head * esz % 16 == 0;
+}
+// few rows: one pass per block, so that the vectors of a row spread over the compute units; many: a row per block
+static dim3 vector_grid(int n_rows, int kv_heads, int lanes)
+{
+    const int passes = (2 * kv_heads * lanes + 255) / 256;
+    return dim3(n_rows, std::max(1, std::min(passes, 2048 / n_rows)));
+}
+
+hipError_t launch_kv8_append(hipStream_t s, const Kv8View &c, const Kv8Rows &rw, int n_rows, int dtype, const void *k, int64_t k_row,
+                             int64_t k_head, const void *v, int64_t v_row, int64_t v_head)
+{
+    const int esz = dtype == SD_BF16 ? 2 : 4, lanes = vector_lanes(c.hd);
+    const bool wide = wide_rows(esz, k, k_row, k_head) && wide_rows(esz, v, v_row, v_head);
+    const dim3 grid = vector_grid(n_rows, c.kv_heads, lanes);
+#define GO(T, W) hipLaunchKernelGGL((kv8_append_kernel<T, W>), grid, dim3(256), 0, s, c, rw, lanes, (const T *)k, k_row, k_head, (const T *)v, v_row, v_head)
+    if (dtype == SD_BF16) {
+        if (wide) GO(bf16_t, true);
+        else GO(bf16_t, false);
+    } else {
+        if (wide) GO(float, true);
+        else GO(float, false);
+    }
+#undef GO
+    return hipGetLastError();
+}
+
+hipError_t launch_kv8_read(hipStream_t s, const Kv8View &c, const Kv8Rows &rw, int n_rows, int dtype, void *k, int64_t k_row, int64_t k_head,
+                           void *v, int64_t v_row, int64_t v_head)
+{
+    const int esz = dtype == SD_BF16 ? 2 : 4, lanes = vector_lanes(c.hd);
+    const bool wide = wide_rows(esz, k, k_row, k_head) && wide_rows(esz, v, v_row, v_head); // (a null pointer counts as aligned)
+    const dim3 grid = vector_grid(n_rows, c.kv_heads, lanes);
+#define GO(T, W) hipLaunchKernelGGL((kv8_read_kernel<T, W>), grid, dim3(256), 0, s, c, rw, lanes, (T *)k, k_row, k_head, (T *)v, v_row, v_head)
+    if (dtype == SD_BF16) {
+        if (wide) GO(bf16_t, true);
+        else GO(bf16_t, false);
+    } else {
+        if (wide) GO(float, true);
+        else GO(float, false);
+    }
+#undef GO
+    return hipGetLastError();
+}
+
+// ---------------------------------------------------------------- the path's step between projection and attention
+// hd / 8 lanes per vector as above, but a lane holds four dimensions of each rotary half, so that a pair never crosses lanes.
+#define KV8_MAX_SLABS 8
+__global__ __launch_bounds__(256) void kv8_rope_append_kernel(const float *__restrict__ qkv, int n_slabs, size_t slab_stride, PlanView pv,
+                                                              CtxView cv, Kv8View c, int lanes, int H, const float2 *__restrict__ rope, int max_pos,
+                                                              float *__restrict__ q, int first)
+{
+    const int r = blockIdx.x, hd = c.hd, half = hd / 2, HD = H * hd;
+    const int pos = pv.row_pos[r];
+    bool valid = pv.row_valid[r];
+    if (pos >= max_pos) {
+        if (threadIdx.x == 0 && blockIdx.y == 0 && valid) atomicOr(cv.status, 8);
+        valid = false;
+    }
+    const int64_t at = cv.off[pv.row_b[r]] + pos;
+    const int per_block = 256 / lanes, l = threadIdx.x & (lanes - 1), d0 = 4 * l, d1 = half + 4 * l;
+    // vectors: the H heads of q (unless first = 1: the rows hold keys and values only), of k, of v
+    const int n = (3 - first) * H;
+    const float *row = qkv + (size_t)r * n * hd;
+    for (int u = blockIdx.y * per_block; u < n; u += gridDim.y * per_block) {
+        const int w = min(u + (int)threadIdx.x / lanes, n - 1), part = w / H + first, h = w % H;
+        const bool live = u + (int)threadIdx.x / lanes < n;
+        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (valid)
+            for (int sl = 0; sl < n_slabs; sl++) { // split-K slabs, added in slab order
+                const float *p = row + (size_t)sl * slab_stride + (size_t)w * hd;
+                const float4 a = *(const float4 *)(p + d0), b = *(const float4 *)(p + d1);
+                x[0] += a.x, x[1] += a.y, x[2] += a.z, x[3] += a.w, x[4] += b.x, x[5] += b.y, x[6] += b.z, x[7] += b.w;
+            }
+        if (valid && part < 2) {
+            const float2 *cs = rope + (size_t)pos * half + d0;
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const float2 t = cs[e];
+                const float a = x[e] * t.x - x[4 + e] * t.y, b = x[4 + e] * t.x + x[e] * t.y;
+                x[e] = a, x[4 + e] = b;
+            }
+        }
+        if (part == 0) {
+            if (live) {
+                float *dst = q + (size_t)r * HD + h * hd;
+                *(float4 *)(dst + d0) = make_float4(x[0], x[1], x[2], x[3]);
+                *(float4 *)(dst + d1) = make_float4(x[4], x[5], x[6], x[7]);
+            }
+        }
+        const float s = kv8_scale(amax_lanes(amax_bits8(x), lanes)), inv = 1.0f / s; // (every lane takes part)
+        if (!valid || !live || part == 0) continue;
+        const bool fine = s == s;
+        const int64_t i = (int64_t)h * c.tokens + at;
+        int8_t *dst = (part == 2 ? c.v : c.k) + i * hd;
+        *(uint32_t *)(dst + d0) = fine ? quantise4(x, s, inv) : 0u;
+        *(uint32_t *)(dst + d1) = fine ? quantise4(x + 4, s, inv) : 0u;
+        if (l == 0) (part == 2 ? c.vs : c.ks)[i] = s;
+    }
+}
+
+hipError_t launch_kv8_rope_append(hipStream_t s, const float *qkv, int n_slabs, size_t slab_stride, PlanView pv, CtxView cv, const Kv8View &c,
+                                  int M, int H, const float2 *rope, int max_pos, float *q, bool kv_only)
+{
+    if (n_slabs > KV8_MAX_SLABS || c.hd < 16 || c.hd > 128 || (c.hd & (c.hd - 1))) return hipErrorInvalidValue; // (the path's head widths: powers of two)
+    const int lanes = c.hd / 8, first = kv_only ? 1 : 0, passes = ((3 - first) * H * lanes + 255) / 256;
+    const dim3 grid(M, std::max(1, std::min(passes, 2048 / M)));
+    hipLaunchKernelGGL(kv8_rope_append_kernel, grid, dim3(256), 0, s, qkv, n_slabs, slab_stride, pv, cv, c, lanes, H, rope, max_pos, q, first);
+    return hipGetLastError();
+}
+
+// ---------------------------------------------------------------- calls
+static int check_cache(const char *who, const sd_kv8 *c)
+{
+    if (!c) return sd_fail(SD_EINVAL, std::string(who) + ": null cache");
+    if (!c->k || !c->v || !c->k_scale || !c->v_scale || !c->off || !c->cap) return sd_fail(SD_EINVAL, std::string(who) + ": null pointer in the cache");
+    if (c->n_kv_heads < 1 || c->n_kv_heads > 65535 || c->n_seq < 1 || c->tokens < 1)
+        return sd_fail(SD_EINVAL, std::string(who) + ": n_kv_heads, n_seq and tokens must be positive");
+    if (c->head_dim < 16 || c->head_dim > 256 || c->head_dim % 16) return sd_fail(SD_EINVAL, std::string(who) + ": head_dim must be a multiple of 16 in 16..256");
+    if (((uintptr_t)c->k | (uintptr_t)c->v) % 16) return sd_fail(SD_EINVAL, std::string(who) + ": codes must be 16-byte aligned");
+    if (((uintptr_t)c->k_scale | (uintptr_t)c->v_scale | (uintptr_t)c->cap | (uintptr_t)c->status) % 4 || (uintptr_t)c->off % 8)
+        return sd_fail(SD_EINVAL, std::string(who) + ": a pointer in the cache is not aligned to its elements");
+    return SD_OK;
+}
+static int check_rows(const char *who, const sd_kv8 *c, const int32_t *len, int n_seq, const int32_t *row_start, int rows)
+{
+    if (!len) return sd_fail(SD_EINVAL, std::string(who) + ": null lengths");
+    if (n_seq < 1 || n_seq > c->n_seq) return sd_fail(SD_EINVAL, std::string(who) + ": n_seq out of range");
+    if (rows < 1 || rows > (1 << 23)) return sd_fail(SD_EINVAL, std::string(who) + ": rows must be 1..2^23"); // (a block per row)
+    if (!row_start && rows % n_seq) return sd_fail(SD_EINVAL, std::string(who) + ": without row_start, rows must be a multiple of n_seq");
+    return SD_OK;
+}
+static int check_strided(const char *who, const char *what, const void *p, int esz, int64_t row, int64_t head, int rows, int heads, int hd)
+{
+    if ((uintptr_t)p % esz) return sd_fail(SD_EINVAL, std::string(who) + ": " + what + " is not aligned to its elements");
+    if ((rows > 1 ? row < hd : row < 0) || (heads > 1 ? head < hd : head < 0))
+        return sd_fail(SD_EINVAL, std::string(who) + ": strides of " + what + " must be at least head_dim");
+    return SD_OK;
+}
+static Kv8View view_of(const sd_kv8 *c)
+{
+    return Kv8View{c->k, c->v, c->k_scale, c->v_scale, c->tokens, c->n_kv_heads, c->head_dim, c->n_seq, c->off, c->cap, c->status};
+}
+static Kv8Rows rows_of(const int32_t *seq_ids, int n_seq, const int32_t *len, const int32_t *row_start, int rows)
+{
+    return Kv8Rows{seq_ids, len, row_start, nullptr, n_seq, row_start ? rows : rows / n_seq, 1, 0};
+}
+
+extern "C" int sd_kv8_append(const sd_kv8 *c, const int32_t *seq_ids, int32_t n_seq, const int32_t *len, const int32_t *row_start,
+                             int32_t rows, int32_t dtype, const void *k, int64_t k_row, int64_t k_head, const void *v, int64_t v_row,
+                             int64_t v_head, void *stream)
+{
+    const char *who = "sd_kv8_append";
+    int rc = check_cache(who, c);
+    if (!rc) rc = check_rows(who, c, len, n_seq, row_start, rows);
+    if (rc) return rc;
+    if (!k || !v) return sd_fail(SD_EINVAL, "sd_kv8_append: null rows");
+    if (dtype != SD_FP32 && dtype != SD_BF16) return sd_fail(SD_EINVAL, "sd_kv8_append: bad dtype");
+    const int esz = dtype == SD_BF16 ? 2 : 4;
+    rc = check_strided(who, "k", k, esz, k_row, k_head, rows, c->n_kv_heads, c->head_dim);
+    if (!rc) rc = check_strided(who, "v", v, esz, v_row, v_head, rows, c->n_kv_heads, c->head_dim);
+    if (rc) return rc;
+    SD_HIP(launch_kv8_append((hipStream_t)stream, view_of(c), rows_of(seq_ids, n_seq, len, row_start, rows), rows, dtype, k, k_row, k_head, v,
+                             v_row, v_head));
+    return SD_OK;
+}
+
+extern "C" int sd_kv8_read(const sd_kv8 *c, const int32_t *seq_ids, int32_t n_seq, const int32_t *start, const int32_t *row_start, int32_t rows,
+                           int32_t dtype, void *k, int64_t k_row, int64_t k_head, void *v, int64_t v_row, int64_t v_head, void *stream)
+{
+    const char *who = "sd_kv8_read";
+    int rc = check_cache(who, c);
+    if (!rc) rc = check_rows(who, c, start, n_seq, row_start, rows);
+    if (rc) return rc;
+    if (!k && !v) return sd_fail(SD_EINVAL, "sd_kv8_read: neither k nor v is wanted");
+    if (dtype != SD_FP32 && dtype != SD_BF16) return sd_fail(SD_EINVAL, "sd_kv8_read: bad dtype");
+    const int esz = dtype == SD_BF16 ? 2 : 4;
+    if (k) rc = check_strided(who, "k", k, esz, k_row, k_head, rows, c->n_kv_heads, c->head_dim);
+    if (!rc && v) rc = check_strided(who, "v", v, esz, v_row, v_head, rows, c->n_kv_heads, c->head_dim);
+    if (rc) return rc;
+    SD_HIP(launch_kv8_read((hipStream_t)stream, view_of(c), rows_of(seq_ids, n_seq, start, row_start, rows), rows, dtype, k, k ? k_row : 0,
+                           k ? k_head : 0, v, v ? v_row : 0, v ? v_head : 0));
+    return SD_OK;
+}
+
+static int check_attn(const char *who, const sd_kv8 *c, const sd_kv8_attn *a)
+{
+    int rc = check_cache(who, c);
+    if (rc) return rc;
+    if (!a) return sd_fail(SD_EINVAL, std::string(who) + ": null arguments");
+    rc = check_rows(who, c, a->len, a->n_seq, a->row_start, a->rows);
+    if (rc) return rc;
+    if (!a->q || !a->out) return sd_fail(SD_EINVAL, std::string(who) + ": null q or out");
+    if (a->dtype != SD_FP32 && a->dtype != SD_BF16) return sd_fail(SD_EINVAL, std::string(who) + ": bad dtype");
+    if (a->n_heads < 1 || a->n_heads > 65535 || a->n_heads % c->n_kv_heads)
+        return sd_fail(SD_EINVAL, std::string(who) + ": n_heads must be a multiple of n_kv_heads");
+    if (a->max_rows < 0 || a->max_len < 0) return sd_fail(SD_EINVAL, std::string(who) + ": max_rows and max_len must not be negative");
+    if (!std::isfinite(a->scale)) return sd_fail(SD_EINVAL, std::string(who) + ": scale must be finite");
+    if (a->window < 0 || a->sinks < 0) return sd_fail(SD_EINVAL, std::string(who) + ": window and sinks must not be negative");
+    if (a->sinks && !a->window) return sd_fail(SD_EINVAL, std::string(who) + ": sinks need a window");
+    if (a->window && !a->causal) return sd_fail(SD_EINVAL, std::string(who) + ": a window needs causal rows");
+    const int esz = a->dtype == SD_BF16 ? 2 : 4;
+    rc = check_strided(who, "q", a->q, esz, a->q_row, a->q_head, a->rows, a->n_heads, c->head_dim);
+    if (!rc) rc = check_strided(who, "out", a->out, esz, a->o_row, a->o_head, a->rows, a->n_heads, c->head_dim);
+    if (rc) return rc;
+    if ((uintptr_t)a->lse % 4) return sd_fail(SD_EINVAL, std::string(who) + ": lse is not aligned to its elements");
+    return SD_OK;
+}
+static Kv8Attn attn_of(const sd_kv8_attn *a)
+{
+    Kv8Attn k = {};
+    k.q = a->q, k.q_row = a->q_row, k.q_head = a->q_head;
+    k.out = a->out, k.o_row = a->o_row, k.o_head = a->o_head;
+    k.lse = a->lse, k.n_heads = a->n_heads, k.dtype = a->dtype;
+    k.causal = a->causal != 0, k.window = a->window, k.sinks = a->sinks;
+    k.scale = a->scale * 1.44269504088896341f;
+    k.total_rows = a->rows, k.max_len = a->max_len;
+    k.max_rows = a->row_start ? a->max_rows : a->rows / a->n_seq;
+    return k;
+}
+
+extern "C" int64_t sd_kv8_attend_workspace(const sd_kv8 *c, const sd_kv8_attn *a)
+{
+    int rc = check_attn("sd_kv8_attend_workspace", c, a);
+    if (rc) return rc;
+    return kv8_attn_workspace(view_of(c), rows_of(a->seq_ids, a->n_seq, a->len, a->row_start, a->rows), attn_of(a));
+}
+
+extern "C" int sd_kv8_attend(const sd_kv8 *c, const sd_kv8_attn *a, void *stream)
+{
+    int rc = check_attn("sd_kv8_attend", c, a);
+    if (rc) return rc;
+    if (a->workspace_bytes < 0 || (uintptr_t)a->workspace % 16) return sd_fail(SD_EINVAL, "sd_kv8_attend: workspace must be 16-byte aligned, its size not negative");
+    const Kv8View v = view_of(c);
+    const Kv8Rows rw = rows_of(a->seq_ids, a->n_seq, a->len, a->row_start, a->rows);
+    const Kv8Attn k = attn_of(a);
+    if (a->workspace && a->workspace_bytes < kv8_attn_workspace(v, rw, k))
+        return sd_fail(SD_ECAP, "sd_kv8_attend: workspace smaller than sd_kv8_attend_workspace says");
+    SD_HIP(launch_kv8_attn((hipStream_t)stream, v, rw, k, a->workspace, a->workspace ? a->workspace_bytes : 0));
+    return SD_OK;
+}

@@ -7,7 +7,7 @@
 #include <memory>
 #include <new>
 
-#include "sd_internal.h"
+#include "kv8.h"
 #include <cmath>
 
 static thread_local std::string g_err;
@@ -210,6 +210,19 @@ extern "C" double sd_alpha_hat(const int32_t *n_accepted, int32_t n_steps, int32
 // ---------------------------------------------------------------- model
 static size_t attn_part_floats(const sd_model_config &c) { return (size_t)3072 * 16 * (c.head_dim + 2); }
 
+// rotary table in double on the host: angle = pos * theta of the pair
+hipError_t set_rope_table(sd_model *m, const double *theta, double gain)
+{
+    const int half = m->cfg.head_dim / 2, max_pos = m->cfg.max_pos;
+    std::vector<float2> tab((size_t)max_pos * half);
+    for (int i = 0; i < half; i++)
+        for (int p = 0; p < max_pos; p++) {
+            double a = p * theta[i];
+            tab[(size_t)p * half + i] = make_float2((float)(gain * cos(a)), (float)(gain * sin(a)));
+        }
+    return hipMemcpy(m->rope, tab.data(), tab.size() * sizeof(float2), hipMemcpyHostToDevice);
+}
+
 extern "C" int sd_load_model(const sd_model_config *cfg, const sd_weights *w, sd_model **out)
 {
     if (!cfg || !w || !out) return sd_fail(SD_EINVAL, "sd_load_model: null argument");
@@ -300,7 +313,7 @@ extern "C" int sd_load_model(const sd_model_config *cfg, const sd_weights *w, sd
     m->logits_stream = nullptr;
     m->logits_device = -1;
     m->lm_norm_rows = 0;
-    m->stopped_at_cache = false;
+    m->stopped_at_cache = m->q_rows = false;
     size_t M = c.max_rows, d = c.d_model;
     m->part_floats = attn_part_floats(c);
     hipError_t e = hipSuccess;
@@ -350,17 +363,9 @@ extern "C" int sd_load_model(const sd_model_config *cfg, const sd_weights *w, sd
     m->plan.seq_kv0 = pm + 6 * M;
     m->plan.seq_nq = pm + 7 * M;
     m->plan.seq_order = pm + 8 * M;
-    // rotary table in double on the host: angle = pos * base^(-2i/hd)
-    int half = c.head_dim / 2;
-    std::vector<float2> tab((size_t)c.max_pos * half);
-    for (int i = 0; i < half; i++) {
-        double theta = pow((double)c.rope_base, -2.0 * i / c.head_dim);
-        for (int p = 0; p < c.max_pos; p++) {
-            double a = p * theta;
-            tab[(size_t)p * half + i] = make_float2((float)cos(a), (float)sin(a));
-        }
-    }
-    SD_HIP(hipMemcpy(m->rope, tab.data(), tab.size() * sizeof(float2), hipMemcpyHostToDevice));
+    double theta[64];
+    for (int i = 0; i < c.head_dim / 2; i++) theta[i] = pow((double)c.rope_base, -2.0 * i / c.head_dim);
+    SD_HIP(set_rope_table(m, theta, 1.0));
     SD_HIP(hipDeviceSynchronize());
     *out = m;
     return SD_OK;
@@ -470,7 +475,10 @@ extern "C" int sd_ctx_create(int32_t batch, const int32_t *caps, sd_ctx **out)
     }
     c->total_cap = tot;
     c->max_cap = *std::max_element(c->cap.begin(), c->cap.end());
-    for (int s = 0; s < SD_MAX_SLOTS; s++) c->models[s] = nullptr, c->kcache[s] = c->vcache[s] = nullptr;
+    for (int s = 0; s < SD_MAX_SLOTS; s++) {
+        c->models[s] = nullptr, c->kcache[s] = c->vcache[s] = nullptr;
+        c->kv8[s] = false, c->kscale[s] = c->vscale[s] = nullptr, c->window[s] = c->sinks[s] = 0;
+    }
     hipError_t e = hipMalloc((void **)&c->d_off, sizeof(int64_t) * batch);
     if (e == hipSuccess) e = hipMalloc((void **)&c->d_cap, sizeof(int32_t) * batch);
     if (e == hipSuccess) e = hipMalloc((void **)&c->d_tokens, sizeof(int32_t) * tot);
@@ -507,6 +515,8 @@ extern "C" int sd_ctx_free(sd_ctx *c)
     for (int s = 0; s < c->n_slots; s++) {
         (void)hipFree(c->kcache[s]);
         (void)hipFree(c->vcache[s]);
+        (void)hipFree(c->kscale[s]);
+        (void)hipFree(c->vscale[s]);
     }
     (void)hipFree(c->d_off);
     (void)hipFree(c->d_cap);
@@ -564,6 +574,46 @@ extern "C" int sd_ctx_attach(sd_ctx *c, sd_model *m)
     c->kcache[s] = k;
     c->vcache[s] = v;
     return SD_OK;
+}
+
+extern "C" int sd_ctx_attach_kv8(sd_ctx *c, sd_model *m, int32_t window, int32_t sinks)
+{
+    if (!c || !m) return sd_fail(SD_EINVAL, "sd_ctx_attach_kv8: null argument");
+    if (window < 0 || sinks < 0) return sd_fail(SD_EINVAL, "sd_ctx_attach_kv8: window and sinks must not be negative");
+    if (sinks && !window) return sd_fail(SD_EINVAL, "sd_ctx_attach_kv8: sinks need a window");
+    const int at = find_slot(c, m);
+    if (at >= 0) {
+        if (c->kv8[at] && c->window[at] == window && c->sinks[at] == sinks) return SD_OK;
+        return sd_fail(SD_EINVAL, "sd_ctx_attach_kv8: model attached already in another form");
+    }
+    if (c->n_slots >= SD_MAX_SLOTS) return sd_fail(SD_ECAP, "sd_ctx_attach_kv8: too many models");
+    const size_t vectors = (size_t)m->cfg.n_layers * m->cfg.n_heads * c->total_cap, bytes[4] = {vectors * m->cfg.head_dim, vectors * m->cfg.head_dim,
+                                                                                               vectors * sizeof(float), vectors * sizeof(float)};
+    void *p[4] = {nullptr, nullptr, nullptr, nullptr}; // codes of K and V, scales of K and V
+    hipError_t e = hipSuccess;
+    for (int i = 0; i < 4; i++) {
+        if (e == hipSuccess) e = hipMalloc(&p[i], bytes[i]);
+        if (e == hipSuccess) e = hipMemset(p[i], 0, bytes[i]); // rows never written stand for zeros
+    }
+    if (e == hipSuccess) e = hipDeviceSynchronize();
+    if (e != hipSuccess) {
+        for (void *q : p) (void)hipFree(q);
+        return sd_fail(SD_EHIP, std::string("sd_ctx_attach_kv8: cache: ") + hipGetErrorString(e));
+    }
+    const int s = c->n_slots++;
+    c->models[s] = m;
+    c->kcache[s] = p[0], c->vcache[s] = p[1], c->kscale[s] = (float *)p[2], c->vscale[s] = (float *)p[3];
+    c->kv8[s] = true, c->window[s] = window, c->sinks[s] = sinks;
+    return SD_OK;
+}
+
+// One layer of slot s as an 8-bit cache.
+static Kv8View kv8_layer(const sd_ctx *c, int s, int layer)
+{
+    const sd_model_config &cf = c->models[s]->cfg;
+    const size_t heads = (size_t)layer * cf.n_heads * c->total_cap;
+    return Kv8View{(int8_t *)c->kcache[s] + heads * cf.head_dim, (int8_t *)c->vcache[s] + heads * cf.head_dim, c->kscale[s] + heads, c->vscale[s] + heads,
+                   c->total_cap, cf.n_heads, cf.head_dim, c->B, c->d_off, c->d_cap, c->d_status};
 }
 
 // One upload and one launch however many sequences: a small copy from pageable memory takes 13 us, and there were twelve per
@@ -652,33 +702,61 @@ extern "C" int sd_ctx_get_tokens(sd_ctx *c, int32_t seq, int32_t *out, int32_t m
     return SD_OK;
 }
 
+// Rows of one layer and sequence to (put) or from the cache, through device staging.
+static int move_kv(const char *who, sd_ctx *c, sd_model *m, int layer, int seq, const void *k_in, const void *v_in, void *k_out, void *v_out, int len)
+{
+    const bool put = k_in != nullptr;
+    int s = find_slot(c, m);
+    if (s < 0) return sd_fail(SD_EINVAL, std::string(who) + ": model not attached");
+    if (layer < 0 || layer >= m->cfg.n_layers || seq < 0 || seq >= c->B) return sd_fail(SD_EINVAL, std::string(who) + ": bad index");
+    if (len < 0 || len > c->cap[seq]) return sd_fail(SD_ECAP, std::string(who) + ": length beyond capacity");
+    if (len == 0) return SD_OK;
+    const int H = m->cfg.n_heads, hd = m->cfg.head_dim, d = m->cfg.d_model;
+    const size_t bytes = (size_t)len * d * m->esz, lstride = (size_t)d * c->total_cap * m->esz;
+    void *dk = nullptr, *dv = nullptr;
+    int32_t *zero = nullptr;
+    hipError_t e = hipDeviceSynchronize();
+    if (e == hipSuccess) e = hipMalloc(&dk, bytes);
+    if (e == hipSuccess) e = hipMalloc(&dv, bytes);
+    if (e == hipSuccess && put) e = hipMemcpy(dk, k_in, bytes, hipMemcpyDefault); // host or device memory
+    if (e == hipSuccess && put) e = hipMemcpy(dv, v_in, bytes, hipMemcpyDefault);
+    if (e == hipSuccess && c->kv8[s]) { // the one sequence, from its first token on
+        e = hipMalloc((void **)&zero, sizeof(int32_t));
+        if (e == hipSuccess) e = hipMemset(zero, 0, sizeof(int32_t));
+        Kv8View v = kv8_layer(c, s, layer);
+        v.n_seq = 1, v.off += seq, v.cap += seq;
+        const Kv8Rows rw = {nullptr, zero, nullptr, nullptr, 1, len, 1, 0};
+        if (e == hipSuccess)
+            e = put ? launch_kv8_append(0, v, rw, len, m->cfg.dtype, dk, d, hd, dv, d, hd) : launch_kv8_read(0, v, rw, len, m->cfg.dtype, dk, d, hd, dv, d, hd);
+    } else if (e == hipSuccess) {
+        char *Kl = (char *)c->kcache[s] + layer * lstride, *Vl = (char *)c->vcache[s] + layer * lstride;
+        e = put ? launch_set_kv(0, m->cfg.dtype, dk, dv, len, H, hd, c->off[seq], c->total_cap, Kl, Vl)
+                : launch_get_kv(0, m->cfg.dtype, dk, dv, len, H, hd, c->off[seq], c->total_cap, Kl, Vl);
+    }
+    if (e == hipSuccess) e = hipDeviceSynchronize();
+    if (e == hipSuccess && !put) e = hipMemcpy(k_out, dk, bytes, hipMemcpyDefault);
+    if (e == hipSuccess && !put) e = hipMemcpy(v_out, dv, bytes, hipMemcpyDefault);
+    (void)hipFree(dk);
+    (void)hipFree(dv);
+    (void)hipFree(zero);
+    if (e != hipSuccess) return sd_fail(SD_EHIP, std::string(who) + ": " + hipGetErrorString(e));
+    return SD_OK;
+}
+
 extern "C" int sd_ctx_set_kv(sd_ctx *c, sd_model *m, int32_t layer, int32_t seq, const void *k, const void *v,
                              int32_t len)
 {
     if (!c || !m || !k || !v) return sd_fail(SD_EINVAL, "sd_ctx_set_kv: null argument");
-    int s = find_slot(c, m);
-    if (s < 0) return sd_fail(SD_EINVAL, "sd_ctx_set_kv: model not attached");
-    if (layer < 0 || layer >= m->cfg.n_layers || seq < 0 || seq >= c->B) return sd_fail(SD_EINVAL, "sd_ctx_set_kv: bad index");
-    if (len < 0 || len > c->cap[seq]) return sd_fail(SD_ECAP, "sd_ctx_set_kv: length beyond capacity");
-    size_t bytes = (size_t)len * m->cfg.d_model * m->esz;
-    void *dk = nullptr, *dv = nullptr;
-    if (len > 0) {
-        SD_HIP(hipMalloc(&dk, bytes));
-        SD_HIP(hipMalloc(&dv, bytes));
-        SD_HIP(hipMemcpy(dk, k, bytes, hipMemcpyDefault)); // host or device source
-        SD_HIP(hipMemcpy(dv, v, bytes, hipMemcpyDefault));
-        size_t lstride = (size_t)m->cfg.d_model * c->total_cap * m->esz;
-        hipError_t e = launch_set_kv(0, m->cfg.dtype, dk, dv, len, m->cfg.n_heads, m->cfg.head_dim, c->off[seq],
-                                     c->total_cap, (char *)c->kcache[s] + layer * lstride,
-                                     (char *)c->vcache[s] + layer * lstride);
-        hipError_t e2 = hipDeviceSynchronize();
-        (void)hipFree(dk);
-        (void)hipFree(dv);
-        SD_HIP(e);
-        SD_HIP(e2);
-    }
-    SD_HIP(hipMemcpy(c->d_kvlen + (size_t)s * c->B + seq, &len, sizeof(int32_t), hipMemcpyHostToDevice));
+    int rc = move_kv("sd_ctx_set_kv", c, m, layer, seq, k, v, nullptr, nullptr, len);
+    if (rc) return rc;
+    SD_HIP(hipMemcpy(c->d_kvlen + (size_t)find_slot(c, m) * c->B + seq, &len, sizeof(int32_t), hipMemcpyHostToDevice));
     return SD_OK;
+}
+
+extern "C" int sd_ctx_get_kv(sd_ctx *c, sd_model *m, int32_t layer, int32_t seq, void *k, void *v, int32_t len)
+{
+    if (!c || !m || !k || !v) return sd_fail(SD_EINVAL, "sd_ctx_get_kv: null argument");
+    return move_kv("sd_ctx_get_kv", c, m, layer, seq, nullptr, nullptr, k, v, len);
 }
 
 extern "C" int sd_ctx_truncate(sd_ctx *c, sd_model *m, int32_t seq, int32_t len)
@@ -754,7 +832,7 @@ extern "C" int sd_debug_read(sd_model *m, const char *name, float *out_host, int
     else if (!strcmp(name, "a")) src = m->abuf;
     else if (!strcmp(name, "act")) src = m->act, w = F, plane = m->plane_f;
     else return sd_fail(SD_EINVAL, "sd_debug_read: unknown buffer");
-    if (m->cfg.dtype == SD_FP32) {
+    if (m->cfg.dtype == SD_FP32 || (src == m->qbuf && m->q_rows)) {
         SD_HIP(hipMemcpy(out_host, src, rows * w * 4, hipMemcpyDeviceToHost));
         return SD_OK;
     }
@@ -924,6 +1002,8 @@ static int forward(sd_model *m, sd_ctx *c, int slot, hipStream_t s, int mode, in
     m->last_a_rows = M;
     m->lm_norm_rows = 0;
     m->stopped_at_cache = cache_only;
+    const bool kv8 = c->kv8[slot];
+    m->q_rows = kv8;
     CtxView cv = c->view();
     PlanView pv = m->plan;
     int kv_upper = std::min(c->len_upper + SD_MAX_GAMMA + 1, c->max_cap);
@@ -1023,15 +1103,32 @@ static int forward(sd_model *m, sd_ctx *c, int slot, hipStream_t s, int mode, in
             if (!qkv_in_place) nq_slabs++;
         }
         if (last_cache) { ProfScope ps(T_ROPE, s);
-            FWD(launch_rope_append(s, cf.dtype, qkv_src, nq_slabs, (size_t)M * n_qkv, pv, cv, M, R, H, hd, m->rope,
+            if (kv8) FWD(launch_kv8_rope_append(s, qkv_src, nq_slabs, (size_t)M * n_qkv, pv, cv, kv8_layer(c, slot, l), M, H, m->rope, cf.max_pos,
+                                                (float *)m->qbuf, kv_only));
+            else FWD(launch_rope_append(s, cf.dtype, qkv_src, nq_slabs, (size_t)M * n_qkv, pv, cv, M, R, H, hd, m->rope,
                                    cf.max_pos, m->qbuf, avd, Kl, Vtl, c->total_cap, kv_only));
             break;
         }
         hipError_t ea = hipErrorNotSupported;
         int oproj_done = 0; // the attention blocks applied the output projection themselves: H slabs in gpart_r
+        if (kv8) {
+            const Kv8View layer = kv8_layer(c, slot, l);
+            { ProfScope ps(T_ROPE, s);
+            FWD(launch_kv8_rope_append(s, qkv_src, nq_slabs, (size_t)M * 3 * d, pv, cv, layer, M, H, m->rope, cf.max_pos, (float *)m->qbuf, false)); }
+            ProfScope ps(T_ATTN, s);
+            const Kv8Rows rw = {pv.seq_b, pv.seq_kv0, nullptr, pv.seq_nq, n_seq, G * R, G, 1};
+            Kv8Attn a = {};
+            a.q = m->qbuf, a.q_row = d, a.q_head = hd;
+            a.out = m->obuf, a.o_row = d, a.o_head = hd, a.out_planes = cf.dtype == SD_BF16, a.av = avd;
+            a.n_heads = H, a.dtype = SD_FP32, a.causal = 1, a.window = c->window[slot], a.sinks = c->sinks[slot];
+            a.scale = 1.44269504088896341f / sqrtf((float)hd);
+            a.total_rows = M, a.max_rows = G * R, a.max_len = kv_upper;
+            ea = launch_kv8_attn(s, layer, rw, a, m->part, (int64_t)(m->part_floats * sizeof(float)));
+            FWD(ea);
+        }
         // RoPE + append + attention in one launch - unless a sequence spans several slots (prefill): their
         // rows must all be in the cache before any slot's attention starts
-        if (cf.dtype == SD_BF16 && !(g_force_generic & 2) && G == 1) {
+        if (!kv8 && cf.dtype == SD_BF16 && !(g_force_generic & 2) && G == 1) {
             ProfScope ps(T_ATTN, s);
             const bool try_oproj = !fold && !lora_o && m->tiled_dd && !(g_force_generic & (1 | 8));
             const bool cached = m->weight_bytes + (size_t)n_seq * kv_upper * cf.n_layers * d * 4 <= ((size_t)256 << 20); // (K and V, 2 bytes each)
@@ -1040,7 +1137,7 @@ static int forward(sd_model *m, sd_ctx *c, int slot, hipStream_t s, int mode, in
                                         m->part_floats, m->arrivals, try_oproj ? m->wo[l] : nullptr, d, m->gpart_r, m->gpart_r_floats, &oproj_done);
             if (ea == hipErrorNotSupported) ps.drop();
         }
-        if (cf.dtype == SD_FP32 && G == 1 && nq_slabs == 1 && !(g_force_generic & (1 | 2))) {
+        if (!kv8 && cf.dtype == SD_FP32 && G == 1 && nq_slabs == 1 && !(g_force_generic & (1 | 2))) {
             ProfScope ps(T_ATTN, s);
             ea = launch_attn_f32_fused(s, qkv_src, m->rope, cf.max_pos, (float *)Kl, (float *)Vtl, pv, cv, R, n_seq, H, hd, c->total_cap, c->max_cap,
                                        (float *)m->qbuf, (float *)m->obuf, avd);

@@ -329,6 +329,7 @@ struct sd_model {
     hipStream_t logits_stream; // where the last forward that writes them was enqueued, and the device then current
     int logits_device;
     int last_lm_rows;
+    bool q_rows; // qbuf holds fp32 rows (the last forward's cache is in 8 bits), whatever the model's type
     bool stopped_at_cache; // the last forward left out what follows the cache append of its last layer
     int last_rows, last_a_rows; // rows of the last forward (layout of the step-major buffers); of abuf
     int lm_norm_rows; // rows of the LM head's input that a norm inside its GEMM kept out of abuf (0: none); sd_debug_read makes them
@@ -349,6 +350,10 @@ struct sd_ctx {
     sd_model *models[SD_MAX_SLOTS];
     void *kcache[SD_MAX_SLOTS];
     void *vcache[SD_MAX_SLOTS];
+    // caches in 8 bits: codes in kcache / vcache, [layer][head][total_cap][head_dim], scales [layer][head][total_cap]
+    bool kv8[SD_MAX_SLOTS];
+    float *kscale[SD_MAX_SLOTS], *vscale[SD_MAX_SLOTS];
+    int32_t window[SD_MAX_SLOTS], sinks[SD_MAX_SLOTS]; // what attention of such a slot sees (0: everything)
     int len_upper; // host upper bound of the longest sequence (tokens): sizes launches, never decides results
     int max_cap;   // largest sequence capacity (tokens)
     CtxView view() const
@@ -378,6 +383,8 @@ int sd_fail(int code, const std::string &s);
         if (e__ != hipSuccess)                                                                \
             return sd_fail(SD_EHIP, std::string(#expr) + ": " + hipGetErrorString(e__));      \
     } while (0)
+
+hipError_t set_rope_table(sd_model *m, const double *theta, double gain); // theta: angle per position of each pair
 
 extern int g_force_generic;
 extern int g_force_tile_cols;  // 96-row GEMM block width forced by option "gemm_tile_cols" (0 = automatic)
@@ -441,6 +448,9 @@ hipError_t launch_route(hipStream_t s, const float *W, const float *b, int n_dra
 hipError_t launch_set_tokens(hipStream_t s, CtxView cv, const int32_t *staged, int n);
 hipError_t launch_set_kv(hipStream_t s, int dtype, const void *k_rows, const void *v_rows, int len, int H, int hd,
                          int64_t seq_off, int64_t total_cap, void *Kl, void *Vtl);
+
+hipError_t launch_get_kv(hipStream_t s, int dtype, void *k_rows, void *v_rows, int len, int H, int hd, int64_t seq_off, int64_t total_cap,
+                         const void *Kl, const void *Vtl);
 
 hipError_t launch_stream_read(hipStream_t s, const void *buf, size_t bytes, uint32_t *out);
 
