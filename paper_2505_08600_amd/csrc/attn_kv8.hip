@@ -2,6 +2,7 @@
 //
 //   s_j = scale * ks_j * (q . kc_j),   out = sum_j exp2(s_j) vs_j vc_j / sum_j exp2(s_j)      (scale in base-2 exponent units)
 #include <algorithm>
+#include <type_traits>
 
 #include "kv8.h"
 
@@ -105,13 +106,460 @@ __global__ __launch_bounds__(256) void kv8_attn_generic_kernel(Kv8View c, Kv8Row
     if (a.lse && tid == 0) a.lse[(int64_t)r * a.n_heads + h] = n ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
 }
 
+// ---------------------------------------------------------------- few rows: one pass over the cache on the matrix cores
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+struct __attribute__((packed, aligned(4))) F4 { // four floats at any element
+    float v[4];
+};
+
+#define K8_TILE 32
+#define K8_P_SHIFT 14 // probabilities enter as p * (vs / E) * 2^14 < 2^15
+
+union Half8 {
+    f16x8 v;
+    f16x2 h[4];
+    uint32_t w[4];
+};
+
+// Eight codes of one token -> eight halves, exactly: with the sign bit flipped a code c is the byte c + 128, and 0x6400 | byte is the
+// half 1024 + byte.
+__device__ __forceinline__ f16x8 codes_to_half(uint32_t a, uint32_t b)
+{
+    Half8 r;
+    const f16x2 bias = {(_Float16)1152.f, (_Float16)1152.f};
+    a ^= 0x80808080u, b ^= 0x80808080u;
+    r.w[0] = __builtin_amdgcn_perm(0x64646464u, a, 0x04010400u);
+    r.w[1] = __builtin_amdgcn_perm(0x64646464u, a, 0x04030402u);
+    r.w[2] = __builtin_amdgcn_perm(0x64646464u, b, 0x04010400u);
+    r.w[3] = __builtin_amdgcn_perm(0x64646464u, b, 0x04030402u);
+#pragma unroll
+    for (int e = 0; e < 4; e++) r.h[e] -= bias;
+    return r.v;
+}
+// Byte j of two words (sign bits flipped) -> two halves (c, c') * 2^-9: as 16-bit integers the bytes are the subnormal halves
+// byte * 2^-24, and byte * 2^-24 * 2^15 - 2^-2 = (byte - 128) * 2^-9 without rounding.
+template <int J>
+__device__ __forceinline__ f16x2 pair_to_half(uint32_t lo, uint32_t hi)
+{
+    const uint32_t u = __builtin_amdgcn_perm(hi, lo, 0x0c000c00u | ((4 + J) << 16) | J);
+    const f16x2 x = __builtin_bit_cast(f16x2, u), m = {(_Float16)32768.f, (_Float16)32768.f}, c = {(_Float16)-0.25f, (_Float16)-0.25f};
+    return __builtin_elementwise_fma(x, m, c);
+}
+// two floats -> two halves, to nearest
+__device__ __forceinline__ f16x2 half2_of(float a, float b)
+{
+    typedef __attribute__((ext_vector_type(2))) float f32x2;
+    const f32x2 v = {a, b};
+    return __builtin_convertvector(v, f16x2);
+}
+
+// Maximum over the four 16-lane rows of a wave, left in every lane (see attn_mfma.hip).
+__device__ __forceinline__ float rows4_max(float v)
+{
+    unsigned u = __float_as_uint(v);
+    const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    u = __float_as_uint(v);
+    const auto b = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float rows4_sum(float v)
+{
+    unsigned u = __float_as_uint(v);
+    const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    u = __float_as_uint(v);
+    const auto b = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// What the rows i0 .. i1 (inclusive) of a sequence see together, in tiles of 32 tokens: first the n_sink tiles from 0 on, then those from
+// w0 on; T in all.  hi_max / lo_min: of any row, hi_min / lo_max: of every row.
+struct Kv8Tiles {
+    int hi_max, hi_min, lo_min, lo_max, n_sink, w0, T;
+    __device__ __forceinline__ int token0(int t) const { return (t < n_sink ? t : w0 + (t - n_sink)) * K8_TILE; }
+};
+__device__ __forceinline__ Kv8Tiles kv8_tiles(const Kv8Attn &a, int len, int i0, int i1, int cap)
+{
+    const Kv8Seen first = kv8_seen(a, len, i0, cap), last = kv8_seen(a, len, i1, cap);
+    Kv8Tiles t;
+    t.hi_max = last.hi, t.hi_min = first.hi, t.lo_min = first.lo, t.lo_max = last.lo;
+    t.w0 = t.lo_min / K8_TILE;
+    t.n_sink = min((a.sinks + K8_TILE - 1) / K8_TILE, t.w0);
+    t.T = t.n_sink + (t.hi_max + K8_TILE - 1) / K8_TILE - t.w0;
+    return t;
+}
+// Tiles per split: an even share, and at least so many that a block has something to stream.
+#define K8_MIN_TILES 16
+__device__ __forceinline__ int kv8_per_split(int T, int S) { return max(K8_MIN_TILES, (T + S - 1) / S); }
+
+// Rows of queries -> the Q^T operands of one 16-row set, scaled by a power of two per row so that the largest element lies in [2^14, 2^15)
+// (halves then hold a bf16 query exactly and two of them 22 bits of a fp32 one).  Lane (qi, grp) takes dimensions 64 j + 16 grp + 8 s
+// .. + 8 into step 2 j + s, the order a 16-byte piece of the codes has them in.  Returns what a product has to be multiplied by.
+template <int HD, int TERMS>
+__device__ __forceinline__ float load_queries(const Kv8Attn &a, bool valid, int64_t at, int grp, f16x8 (&q)[TERMS][HD / 32])
+{
+    float x[HD / 4];
+    float mx = 0.f;
+#pragma unroll
+    for (int j = 0; j < HD / 64; j++) {
+        const int64_t p = at + 64 * j + 16 * grp;
+#pragma unroll
+        for (int e = 0; e < 16; e++) {
+            float v = 0.f;
+            if (valid) v = TERMS == 1 ? to_float(((const bf16_t *)a.q)[p + e]) : ((const float *)a.q)[p + e];
+            x[16 * j + e] = v;
+            mx = fmaxf(mx, fabsf(v));
+        }
+    }
+    mx = rows4_max(mx);
+    // exponent e with 2^e <= mx < 2^(e+1), kept where both factors are normal numbers
+    const int e = min(127, max(-100, (int)(__float_as_uint(mx) >> 23) - 127));
+    const float up = __uint_as_float((uint32_t)(127 + 14 - e) << 23), down = __uint_as_float((uint32_t)max(1, 127 - 14 + e) << 23);
+#pragma unroll
+    for (int s = 0; s < HD / 32; s++) {
+        Half8 hi, lo;
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            const float u = x[8 * s + 2 * k] * up, v = x[8 * s + 2 * k + 1] * up;
+            hi.h[k] = half2_of(u, v);
+            if (TERMS == 2) lo.h[k] = half2_of(u - (float)hi.h[k][0], v - (float)hi.h[k][1]);
+        }
+        q[0][s] = hi.v;
+        if constexpr (TERMS == 2) q[1][s] = lo.v;
+    }
+    return down * a.scale;
+}
+
+// One wave's share of a tile's bytes, in flight while the tile before it is consumed.
+template <int HD>
+struct K8Regs {
+    struct __attribute__((aligned(HD / 16))) VRow { // a lane's words of a V row
+        uint32_t w[HD / 64];
+    };
+    uint4 k[2][HD / 64];
+    VRow v[8];
+    F4 ks[2], vs[2]; // tokens 4 grp .. + 4 and 16 + 4 grp .. + 4
+};
+
+// Block: 4 waves over the tiles of one (sequence, cache head, set of MT * 16 rows, split), each with a running softmax of its own.
+//   S^T = K Q^T: two operands of 16 tokens each, read from the codes' rows in 16-byte pieces.  The result leaves lane (qi, grp)
+//   tokens 4 grp + r of both halves for row qi, which are the eight k-slots of the P^T operand of
+//   O^T = V^T P^T: V's rows are read as they lie (lane (m, grp): VB dimensions from VB m on of eight tokens) and transposed by
+//   the byte permutes that widen them.
+// E, a power of two above half the largest V scale so far, takes the scales' range out of the 16-bit probabilities.
+// Bound: memory; per code about 1.2 vector operations to widen it, beside one matrix instruction per 512 codes and 16 rows.
+template <int HD, int MT, int TERMS>
+__global__ __launch_bounds__(256, MT == 1 ? 2 : 1) void kv8_attn_stream_kernel(Kv8View c, Kv8Rows rw, Kv8Attn a, int n_chunks, int S, float *part)
+{
+    constexpr int NS = HD / 32, VB = HD / 16, VW = HD / 64, ND = VB;
+    constexpr int DP = HD < 128 ? HD : 128; // dimensions merged at a time
+    __shared__ float sO[4][DP * 17];
+    __shared__ float sM[4][16], sL[4][16];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int qi = lane & 15, grp = lane >> 4;
+    const int kvh = blockIdx.x % c.kv_heads, j = blockIdx.x / c.kv_heads % rw.n, chunk0 = blockIdx.x / c.kv_heads / rw.n, split = blockIdx.y;
+    const Kv8Seq sq = kv8_seq(c, rw, j);
+    const int grps = a.n_heads / c.kv_heads;
+    if (sq.b < 0 && c.status && threadIdx.x == 0) atomicOr(c.status, 4);
+    const int n_rows = sq.b < 0 ? 0 : sq.n_rows;
+    const int64_t all = (int64_t)(rw.path ? rw.rows : n_rows) * grps; // (unused slots of the path receive zeros)
+    const int cap = sq.b < 0 ? 0 : c.cap[sq.b];
+    const int64_t base = (int64_t)kvh * c.tokens + (sq.b < 0 ? 0 : c.off[sq.b]);
+    const int8_t *K = c.k + base * HD, *V = c.v + base * HD;
+    const float *KS = c.ks + base, *VS = c.vs + base;
+    for (int64_t m0 = (int64_t)chunk0 * MT * 16; m0 < all; m0 += (int64_t)n_chunks * MT * 16) {
+        const int i_first = (int)(m0 / grps), i_last = (int)min((int64_t)n_rows - 1, (m0 + MT * 16 - 1) / grps);
+        Kv8Tiles tl = {};
+        if (i_first < n_rows) tl = kv8_tiles(a, sq.len, i_first, i_last, cap);
+        const int per = kv8_per_split(tl.T, S), t_begin = split * per, t_end = min(tl.T, t_begin + per);
+        if (split > 0 && t_begin >= tl.T) continue;
+        // the lane's row in each set
+        f16x8 q[MT][TERMS][NS];
+        float qf[MT], m_run[MT], l_run[MT];
+        Kv8Seen seen[MT];
+        f32x4 o[MT][ND];
+#pragma unroll
+        for (int mt = 0; mt < MT; mt++) {
+            const int64_t m = m0 + 16 * mt + qi;
+            const int i = (int)(m / grps), g = (int)(m % grps);
+            const bool valid = i < n_rows;
+            seen[mt] = kv8_seen(a, sq.len, i, cap);
+            if (!valid) seen[mt] = Kv8Seen{0, 0, 0};
+            qf[mt] = load_queries<HD, TERMS>(a, valid, (int64_t)(sq.row0 + i) * a.q_row + (int64_t)(kvh * grps + g) * a.q_head, grp, q[mt]);
+            m_run[mt] = -INFINITY, l_run[mt] = 0.f;
+#pragma unroll
+            for (int d = 0; d < ND; d++) o[mt][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        float E = KV8_SCALE_MIN;
+        const int last_tok = max(0, tl.hi_max - 1);
+        const uint32_t k_lane = qi * HD + 16 * grp, v_lane = 4 * grp * HD + VB * qi; // byte offsets of the lane inside a tile
+        auto load = [&](int t, K8Regs<HD> &r) {
+            const int t0 = tl.token0(t);
+            if (t0 + K8_TILE <= tl.hi_max) { // (uniform) a whole tile: one address and constant offsets
+                const int8_t *kt = K + (int64_t)t0 * HD, *vt = V + (int64_t)t0 * HD;
+#pragma unroll
+                for (int h = 0; h < 2; h++)
+#pragma unroll
+                    for (int p = 0; p < HD / 64; p++) r.k[h][p] = *(const uint4 *)(kt + k_lane + (16 * h * HD + 64 * p));
+#pragma unroll
+                for (int e = 0; e < 8; e++)
+                    r.v[e] = *(const typename K8Regs<HD>::VRow *)(vt + v_lane + (e < 4 ? e : 12 + e) * HD);
+#pragma unroll
+                for (int h = 0; h < 2; h++) r.ks[h] = *(const F4 *)(KS + t0 + 16 * h + 4 * grp), r.vs[h] = *(const F4 *)(VS + t0 + 16 * h + 4 * grp);
+            } else { // tokens behind the last one any row sees repeat that one
+#pragma unroll
+                for (int h = 0; h < 2; h++)
+#pragma unroll
+                    for (int p = 0; p < HD / 64; p++) r.k[h][p] = *(const uint4 *)(K + (int64_t)min(t0 + 16 * h + qi, last_tok) * HD + 64 * p + 16 * grp);
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    const int tok = min(t0 + 16 * (e / 4) + 4 * grp + e % 4, last_tok);
+                    r.v[e] = *(const typename K8Regs<HD>::VRow *)(V + (int64_t)tok * HD + VB * qi);
+                    r.ks[e / 4].v[e % 4] = KS[tok], r.vs[e / 4].v[e % 4] = VS[tok];
+                }
+            }
+        };
+        auto consume = [&](int t, const K8Regs<HD> &r, auto masked) {
+            constexpr bool MASKED = decltype(masked)::value;
+            const int t0 = tl.token0(t);
+            f32x4 s[MT][2];
+#pragma unroll
+            for (int mt = 0; mt < MT; mt++) s[mt][0] = s[mt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int h = 0; h < 2; h++)
+#pragma unroll
+                for (int p = 0; p < HD / 64; p++) {
+                    const f16x8 k0 = codes_to_half(r.k[h][p].x, r.k[h][p].y), k1 = codes_to_half(r.k[h][p].z, r.k[h][p].w);
+#pragma unroll
+                    for (int mt = 0; mt < MT; mt++)
+#pragma unroll
+                        for (int w = 0; w < TERMS; w++) {
+                            s[mt][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, q[mt][w][2 * p], s[mt][h], 0, 0, 0);
+                            s[mt][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, q[mt][w][2 * p + 1], s[mt][h], 0, 0, 0);
+                        }
+                }
+            __builtin_amdgcn_sched_barrier(0);
+            // the tile's V scales over E
+            float vs[8], big = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                vs[e] = r.vs[e / 4].v[e % 4];
+                if (MASKED) { // scales of tokens that no row sees are not looked at
+                    const int tok = t0 + 16 * (e / 4) + 4 * grp + e % 4;
+                    if (!(tok < tl.hi_max && (tok >= tl.lo_min || tok < a.sinks))) vs[e] = 0.f;
+                }
+                big = fmaxf(big, vs[e]);
+            }
+            big = __uint_as_float(min(__float_as_uint(rows4_max(big)), 0x7e000000u) & 0x7f800000u);
+            const float E_new = fmaxf(E, big);
+            const float inv = __uint_as_float(0x7f000000u + (K8_P_SHIFT << 23) - __float_as_uint(E_new));
+            const float shrink = E * __uint_as_float(0x7f000000u - __float_as_uint(E_new));
+            E = E_new;
+#pragma unroll
+            for (int e = 0; e < 8; e++) vs[e] *= inv;
+            Half8 ph[MT][TERMS];
+#pragma unroll
+            for (int mt = 0; mt < MT; mt++) {
+                float x[8], mx = -INFINITY;
+                bool vis[8];
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    x[e] = s[mt][e / 4][e % 4] * r.ks[e / 4].v[e % 4] * qf[mt];
+                    if (MASKED) {
+                        const int tok = t0 + 16 * (e / 4) + 4 * grp + e % 4;
+                        vis[e] = tok < seen[mt].hi && (tok >= seen[mt].lo || tok < a.sinks);
+                        x[e] = vis[e] ? x[e] : -INFINITY;
+                    }
+                    mx = fmaxf(mx, x[e]);
+                }
+                const float m_new = fmaxf(m_run[mt], rows4_max(mx));
+                const float ref = m_new == -INFINITY ? 0.f : m_new;
+                const float corr = __builtin_amdgcn_exp2f(m_run[mt] - ref), corr_o = corr * shrink;
+                m_run[mt] = m_new;
+                float sum = 0.f;
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    float p[2];
+#pragma unroll
+                    for (int f = 0; f < 2; f++) {
+                        p[f] = __builtin_amdgcn_exp2f(x[e + f] - ref);
+                        sum += p[f];
+                        p[f] *= vs[e + f];
+                        if (MASKED) p[f] = vis[e + f] ? p[f] : 0.f;
+                    }
+                    ph[mt][0].h[e / 2] = half2_of(p[0], p[1]);
+                    if constexpr (TERMS == 2)
+                        ph[mt][1].h[e / 2] = half2_of(p[0] - (float)ph[mt][0].h[e / 2][0], p[1] - (float)ph[mt][0].h[e / 2][1]);
+                }
+                l_run[mt] = l_run[mt] * corr + sum;
+                if (__any(corr_o != 1.0f)) {
+                    asm volatile("" ::: "memory");
+#pragma unroll
+                    for (int d = 0; d < ND; d++) o[mt][d] *= corr_o;
+                }
+            }
+            // V^T fragments, byte by byte of the words
+            __builtin_amdgcn_sched_barrier(0); // (widened early, the fragments would cost a second set of registers)
+#pragma unroll
+            for (int w = 0; w < VW; w++) {
+                Half8 f[4];
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const uint32_t a0 = r.v[2 * e].w[w] ^ 0x80808080u, a1 = r.v[2 * e + 1].w[w] ^ 0x80808080u;
+                    f[0].h[e] = pair_to_half<0>(a0, a1);
+                    f[1].h[e] = pair_to_half<1>(a0, a1);
+                    f[2].h[e] = pair_to_half<2>(a0, a1);
+                    f[3].h[e] = pair_to_half<3>(a0, a1);
+                }
+#pragma unroll
+                for (int b = 0; b < 4; b++)
+#pragma unroll
+                    for (int mt = 0; mt < MT; mt++)
+#pragma unroll
+                        for (int u = 0; u < TERMS; u++)
+                            o[mt][4 * w + b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[b].v, ph[mt][u].v, o[mt][4 * w + b], 0, 0, 0);
+            }
+        };
+        if (t_begin + wave < t_end) {
+            K8Regs<HD> cur, next;
+            load(t_begin + wave, cur);
+            for (int t = t_begin + wave; t < t_end; t += 4) {
+                if (t + 4 < t_end) load(t + 4, next);
+                __builtin_amdgcn_sched_barrier(0);
+                const int t0 = tl.token0(t);
+                if (t0 + K8_TILE <= tl.hi_min && (t0 >= tl.lo_max || t0 + K8_TILE <= a.sinks)) consume(t, cur, std::false_type{});
+                else consume(t, cur, std::true_type{});
+                cur = next;
+            }
+        }
+        // the waves' parts meet: O in true units (E and the shifts undone), weighted by their maxima
+        const float unit = E * 0.03125f; // 2^(9 - 14)
+#pragma unroll
+        for (int mt = 0; mt < MT; mt++) {
+            const float l = rows4_sum(l_run[mt]);
+#pragma unroll
+            for (int d0 = 0; d0 < HD; d0 += DP) { // (a pass holds the accumulators of VB / (HD / DP) bytes of each lane's dimensions)
+                __syncthreads();
+                if (grp == 0 && d0 == 0) sM[wave][qi] = m_run[mt], sL[wave][qi] = l;
+                constexpr int NB = VB / (HD / DP);
+#pragma unroll
+                for (int b = 0; b < NB; b++)
+#pragma unroll
+                    for (int r = 0; r < 4; r++) sO[wave][(NB * (4 * grp + r) + b) * 17 + qi] = o[mt][d0 / DP * NB + b][r] * unit;
+                __syncthreads();
+                for (int u = threadIdx.x; u < DP * 16; u += 256) {
+                    const int dd = u % DP, row = u / DP;
+                    const int d = VB * (dd / NB) + d0 / DP * NB + dd % NB;
+                    const int64_t m = m0 + 16 * mt + row;
+                    if (m >= all) continue;
+                    const float M = fmaxf(fmaxf(sM[0][row], sM[1][row]), fmaxf(sM[2][row], sM[3][row])), ref = M == -INFINITY ? 0.f : M;
+                    float O = 0.f, L = 0.f;
+#pragma unroll
+                    for (int w = 0; w < 4; w++) {
+                        const float f = __builtin_amdgcn_exp2f(sM[w][row] - ref);
+                        O += sO[w][dd * 17 + row] * f;
+                        L += sL[w][row] * f;
+                    }
+                    const int i = (int)(m / grps), h = kvh * grps + (int)(m % grps), r = sq.row0 + i;
+                    if (tl.T <= per) { // one split: this is the result
+                        // (nothing seen: L is 0.  A sum that is not a number stays one.)
+                        kv8_store_out(a, r, h, HD, d, L == 0.f ? 0.f : O / L);
+                        if (a.lse && d == 0) a.lse[(int64_t)r * a.n_heads + h] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
+                    } else {
+                        float *p = part + (((int64_t)r * a.n_heads + h) * S + split) * (HD + 4);
+                        p[4 + d] = O;
+                        if (d == 0) p[0] = M, p[1] = L;
+                    }
+                }
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// Joins the splits of one (row, head).
+template <int HD>
+__global__ __launch_bounds__(HD) void kv8_attn_join_kernel(Kv8View c, Kv8Rows rw, Kv8Attn a, int set_rows, int S, const float *__restrict__ part)
+{
+    const int r = blockIdx.x, h = blockIdx.y, d = threadIdx.x;
+    const int j = kv8_owner(rw, r);
+    if (j < 0 || j >= rw.n) return;
+    const Kv8Seq sq = kv8_seq(c, rw, j);
+    const int i = r - sq.row0, grps = a.n_heads / c.kv_heads;
+    if (sq.b < 0 || i >= sq.n_rows) return;
+    const int64_t m0 = ((int64_t)i * grps + h % grps) / set_rows * set_rows; // the set of rows that the row went with
+    const int i_last = (int)min((int64_t)sq.n_rows - 1, (m0 + set_rows - 1) / grps);
+    const int T = kv8_tiles(a, sq.len, (int)(m0 / grps), i_last, c.cap[sq.b]).T, per = kv8_per_split(T, S), used = (T + per - 1) / per;
+    if (used <= 1) return; // the block has written the result
+    const float *p = part + ((int64_t)r * a.n_heads + h) * S * (HD + 4);
+    float M = -INFINITY;
+    for (int s = 0; s < used; s++) M = fmaxf(M, p[s * (HD + 4)]);
+    const float ref = M == -INFINITY ? 0.f : M;
+    float O = 0.f, L = 0.f;
+    for (int s = 0; s < used; s++) {
+        const float f = __builtin_amdgcn_exp2f(p[s * (HD + 4)] - ref);
+        O += p[s * (HD + 4) + 4 + d] * f;
+        L += p[s * (HD + 4) + 1] * f;
+    }
+    kv8_store_out(a, r, h, HD, d, L == 0.f ? 0.f : O / L);
+    if (a.lse && d == 0) a.lse[(int64_t)r * a.n_heads + h] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
+}
+
+// ---------------------------------------------------------------- which kernel, how many blocks
+struct Kv8Plan {
+    bool stream;
+    int mt, chunks, splits;
+};
+static Kv8Plan kv8_plan(const Kv8View &c, const Kv8Rows &rw, const Kv8Attn &a, int64_t ws_bytes)
+{
+    Kv8Plan p = {};
+    if ((g_force_generic & 2) || (c.hd != 64 && c.hd != 128)) return p;
+    p.stream = true;
+    const int64_t max_rows = a.max_rows > 0 ? std::min(a.max_rows, a.total_rows) : a.total_rows;
+    const int64_t R = max_rows * (a.n_heads / c.kv_heads); // rows of the products
+    p.mt = R <= 16 ? 1 : 2;
+    p.chunks = (int)std::min<int64_t>((R + 16 * p.mt - 1) / (16 * p.mt), 4096);
+    // splits: about four blocks for each of the 256 compute units, each with K8_MIN_TILES tiles at least
+    const int64_t blocks = (int64_t)rw.n * c.kv_heads * p.chunks;
+    const int64_t tokens = a.window ? std::min<int64_t>((int64_t)a.window + a.sinks + max_rows, (int64_t)a.max_len + max_rows) : (int64_t)a.max_len + max_rows;
+    const int64_t tiles = (tokens + K8_TILE - 1) / K8_TILE;
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(64, (tiles + K8_MIN_TILES - 1) / K8_MIN_TILES), (1024 + blocks - 1) / blocks));
+    const int64_t one = (int64_t)a.total_rows * a.n_heads * (c.hd + 4) * sizeof(float);
+    if (ws_bytes >= 0 && p.splits > 1) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(p.splits, ws_bytes / one));
+    return p;
+}
+
 int64_t kv8_attn_workspace(const Kv8View &c, const Kv8Rows &rw, const Kv8Attn &a)
 {
-    return 0;
+    const Kv8Plan p = kv8_plan(c, rw, a, -1);
+    return p.stream && p.splits > 1 ? (int64_t)a.total_rows * a.n_heads * (c.hd + 4) * sizeof(float) * p.splits : 0;
+}
+
+template <int HD>
+static void stream_launch(hipStream_t s, const Kv8Plan &p, const Kv8View &c, const Kv8Rows &rw, const Kv8Attn &a, float *part)
+{
+    const dim3 grid((unsigned)((int64_t)rw.n * c.kv_heads * p.chunks), p.splits);
+#define GO(MT, T) hipLaunchKernelGGL((kv8_attn_stream_kernel<HD, MT, T>), grid, dim3(256), 0, s, c, rw, a, p.chunks, p.splits, part)
+    if (a.dtype == SD_BF16) {
+        if (p.mt == 1) GO(1, 1);
+        else GO(2, 1);
+    } else {
+        if (p.mt == 1) GO(1, 2);
+        else GO(2, 2);
+    }
+#undef GO
+    if (p.splits > 1)
+        hipLaunchKernelGGL(kv8_attn_join_kernel<HD>, dim3(a.total_rows, a.n_heads), dim3(HD), 0, s, c, rw, a, 16 * p.mt, p.splits, part);
 }
 
 hipError_t launch_kv8_attn(hipStream_t s, const Kv8View &c, const Kv8Rows &rw, const Kv8Attn &a, void *ws, int64_t ws_bytes)
 {
-    hipLaunchKernelGGL(kv8_attn_generic_kernel, dim3(a.total_rows, a.n_heads), dim3(256), 0, s, c, rw, a);
+    const Kv8Plan p = kv8_plan(c, rw, a, ws_bytes);
+    if (!p.stream) hipLaunchKernelGGL(kv8_attn_generic_kernel, dim3(a.total_rows, a.n_heads), dim3(256), 0, s, c, rw, a);
+    else if (c.hd == 64) stream_launch<64>(s, p, c, rw, a, (float *)ws);
+    else stream_launch<128>(s, p, c, rw, a, (float *)ws);
     return hipGetLastError();
 }

@@ -47,6 +47,8 @@ __device__ __forceinline__ Kv8Seq kv8_seq(const Kv8View &c, const Kv8Rows &rw, i
         for (int o = 32; o; o >>= 1) t += __shfl_xor(t, o, 64);
         s.n_rows = t;
     }
+    s.b = __builtin_amdgcn_readfirstlane(s.b), s.len = __builtin_amdgcn_readfirstlane(s.len);
+    s.row0 = __builtin_amdgcn_readfirstlane(s.row0), s.n_rows = __builtin_amdgcn_readfirstlane(s.n_rows);
     return s;
 }
 
