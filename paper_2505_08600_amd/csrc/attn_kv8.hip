@@ -27,6 +27,33 @@ __device__ __forceinline__ void kv8_store_out(const Kv8Attn &a, int r, int h, in
     else ((float *)a.out)[r * a.o_row + h * a.o_head + d] = v;
 }
 
+// N (4 or 8) adjacent dimensions of one (row, head), d a multiple of N.  wide: rows of out allow 16-byte accesses.
+template <int N>
+__device__ __forceinline__ void kv8_store_run(const Kv8Attn &a, bool wide, int r, int h, int hd, int d, const float (&v)[N])
+{
+    if (a.out_planes) {
+#pragma unroll
+        for (int e = 0; e < N; e += 4)
+            store_act4((bf16_t *)a.out, act_index(a.av, r, h * hd + d + e, a.n_heads * hd), a.av.plane, v[e], v[e + 1], v[e + 2], v[e + 3]);
+    } else if (!wide) {
+#pragma unroll
+        for (int e = 0; e < N; e++) kv8_store_out(a, r, h, hd, d + e, v[e]);
+    } else if (a.dtype == SD_BF16) {
+        bf16_t *p = (bf16_t *)a.out + (r * a.o_row + h * a.o_head + d);
+#pragma unroll
+        for (int e = 0; e < N; e += 4) *(uint2 *)(p + e) = make_uint2(bf16x2_bits_rne(v[e], v[e + 1]), bf16x2_bits_rne(v[e + 2], v[e + 3]));
+    } else {
+        float *p = (float *)a.out + (r * a.o_row + h * a.o_head + d);
+#pragma unroll
+        for (int e = 0; e < N; e += 4) *(float4 *)(p + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+    }
+}
+__device__ __forceinline__ bool kv8_wide(const void *p, int64_t row, int64_t head, int dtype)
+{
+    const int64_t n = dtype == SD_BF16 ? 8 : 4;
+    return (uintptr_t)p % 16 == 0 && row % n == 0 && head % n == 0;
+}
+
 // ---------------------------------------------------------------- the plain kernel
 // One block per (row, head), every head width; 32-bit arithmetic throughout.  A chunk of 256 tokens at a time: a thread per token
 // for the scores, then threads over dimensions and token groups for the output.
@@ -195,29 +222,54 @@ __device__ __forceinline__ Kv8Tiles kv8_tiles(const Kv8Attn &a, int len, int i0,
 #define K8_MIN_TILES 16
 __device__ __forceinline__ int kv8_per_split(int T, int S) { return max(K8_MIN_TILES, (T + S - 1) / S); }
 
-// Rows of queries -> the Q^T operands of one 16-row set, scaled by a power of two per row so that the largest element lies in [2^14, 2^15)
-// (halves then hold a bf16 query exactly and two of them 22 bits of a fp32 one).  Lane (qi, grp) takes dimensions 64 j + 16 grp + 8 s
-// .. + 8 into step 2 j + s, the order a 16-byte piece of the codes has them in.  Returns what a product has to be multiplied by.
-template <int HD, int TERMS>
-__device__ __forceinline__ float load_queries(const Kv8Attn &a, bool valid, int64_t at, int grp, f16x8 (&q)[TERMS][HD / 32])
+// 16 adjacent elements of a query row
+template <int TERMS>
+__device__ __forceinline__ void load_q16(const Kv8Attn &a, bool wide, int64_t at, float *x)
 {
-    float x[HD / 4];
-    float mx = 0.f;
+    if constexpr (TERMS == 1) {
+        const bf16_t *p = (const bf16_t *)a.q + at;
+        if (wide) {
 #pragma unroll
-    for (int j = 0; j < HD / 64; j++) {
-        const int64_t p = at + 64 * j + 16 * grp;
+            for (int v = 0; v < 2; v++) {
+                const uint4 w = ((const uint4 *)p)[v];
+                const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-        for (int e = 0; e < 16; e++) {
-            float v = 0.f;
-            if (valid) v = TERMS == 1 ? to_float(((const bf16_t *)a.q)[p + e]) : ((const float *)a.q)[p + e];
-            x[16 * j + e] = v;
-            mx = fmaxf(mx, fabsf(v));
+                for (int e = 0; e < 4; e++) x[8 * v + 2 * e] = __uint_as_float(u[e] << 16), x[8 * v + 2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16; e++) x[e] = to_float(p[e]);
+        }
+    } else {
+        const float *p = (const float *)a.q + at;
+        if (wide) {
+#pragma unroll
+            for (int v = 0; v < 4; v++) {
+                const float4 w = ((const float4 *)p)[v];
+                x[4 * v] = w.x, x[4 * v + 1] = w.y, x[4 * v + 2] = w.z, x[4 * v + 3] = w.w;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16; e++) x[e] = p[e];
         }
     }
-    mx = rows4_max(mx);
-    // exponent e with 2^e <= mx < 2^(e+1), kept where both factors are normal numbers
-    const int e = min(127, max(-100, (int)(__float_as_uint(mx) >> 23) - 127));
-    const float up = __uint_as_float((uint32_t)(127 + 14 - e) << 23), down = __uint_as_float((uint32_t)max(1, 127 - 14 + e) << 23);
+}
+// Queries enter the products as halves.  They are scaled by one power of two for all rows that share it, so that the largest element
+// (mx) lies in [2^14, 2^15): a half then holds every bf16 element down to 2^-31 of the largest exactly, two halves hold 22 bits of an
+// fp32 one, and what smaller elements lose is 2^-39 of the largest - nothing in a score.
+struct QScale {
+    float up, down; // to the halves, and back
+};
+__device__ __forceinline__ QScale q_scale(float mx)
+{
+    const int e = min(127, max(-100, (int)(__float_as_uint(mx) >> 23) - 127)); // (kept where both factors are normal numbers)
+    return QScale{__uint_as_float((uint32_t)(127 + 14 - e) << 23), __uint_as_float((uint32_t)(127 - 14 + e) << 23)};
+}
+// The Q^T operands of a 16-row set: lane (qi, grp) takes dimensions 64 j + 16 grp + 8 s .. + 8 into step 2 j + s, the order a 16-byte
+// piece of the codes has them in.
+template <int HD, int TERMS>
+__device__ __forceinline__ void query_operands(const float (&x)[HD / 4], float up, f16x8 (&q)[TERMS][HD / 32])
+{
 #pragma unroll
     for (int s = 0; s < HD / 32; s++) {
         Half8 hi, lo;
@@ -230,7 +282,40 @@ __device__ __forceinline__ float load_queries(const Kv8Attn &a, bool valid, int6
         q[0][s] = hi.v;
         if constexpr (TERMS == 2) q[1][s] = lo.v;
     }
-    return down * a.scale;
+}
+// MT sets of 16 rows from product row m0 on (row i, head g of the group: m = i * grps + g); returns what a product has to be multiplied
+// by to be a score.
+template <int HD, int MT, int TERMS, typename MX>
+__device__ __forceinline__ float load_queries(const Kv8Attn &a, const Kv8Seq &sq, int n_rows, int kvh, int grps, int64_t m0, f16x8 (&q)[MT][TERMS][HD / 32],
+                                              MX all_max)
+{
+    const int qi = threadIdx.x & 15, grp = (threadIdx.x & 63) >> 4;
+    const bool wide = kv8_wide(a.q, a.q_row, a.q_head, a.dtype);
+    float x[MT][HD / 4], mx = 0.f;
+#pragma unroll
+    for (int mt = 0; mt < MT; mt++) {
+        const int64_t m = m0 + 16 * mt + qi;
+        const int i = (int)(m / grps), g = (int)(m % grps);
+#pragma unroll
+        for (int e = 0; e < HD / 4; e++) x[mt][e] = 0.f;
+        if (i < n_rows) {
+            const int64_t at = (int64_t)(sq.row0 + i) * a.q_row + (int64_t)(kvh * grps + g) * a.q_head;
+#pragma unroll
+            for (int j = 0; j < HD / 64; j++) load_q16<TERMS>(a, wide, at + 64 * j + 16 * grp, &x[mt][16 * j]);
+        }
+#pragma unroll
+        for (int e = 0; e < HD / 4; e++) mx = fmaxf(mx, fabsf(x[mt][e]));
+    }
+    const QScale qs = q_scale(all_max(mx));
+#pragma unroll
+    for (int mt = 0; mt < MT; mt++) query_operands<HD, TERMS>(x[mt], qs.up, q[mt]);
+    return qs.down * a.scale;
+}
+// over the wave
+__device__ __forceinline__ float wave_max(float v)
+{
+    for (int o = 32; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+    return v;
 }
 
 // One wave's share of a tile's bytes, in flight while the tile before it is consumed.
@@ -276,19 +361,16 @@ __global__ __launch_bounds__(256, MT == 1 ? 2 : 1) void kv8_attn_stream_kernel(K
         if (i_first < n_rows) tl = kv8_tiles(a, sq.len, i_first, i_last, cap);
         const int per = kv8_per_split(tl.T, S), t_begin = split * per, t_end = min(tl.T, t_begin + per);
         if (split > 0 && t_begin >= tl.T) continue;
-        // the lane's row in each set
         f16x8 q[MT][TERMS][NS];
-        float qf[MT], m_run[MT], l_run[MT];
-        Kv8Seen seen[MT];
+        const float qf = load_queries<HD, MT, TERMS>(a, sq, n_rows, kvh, grps, m0, q, wave_max); // (the same for every wave: they hold the same rows)
+        float m_run[MT], l_run[MT];
+        Kv8Seen seen[MT]; // of the lane's row in each set
         f32x4 o[MT][ND];
 #pragma unroll
         for (int mt = 0; mt < MT; mt++) {
-            const int64_t m = m0 + 16 * mt + qi;
-            const int i = (int)(m / grps), g = (int)(m % grps);
-            const bool valid = i < n_rows;
+            const int i = (int)((m0 + 16 * mt + qi) / grps);
             seen[mt] = kv8_seen(a, sq.len, i, cap);
-            if (!valid) seen[mt] = Kv8Seen{0, 0, 0};
-            qf[mt] = load_queries<HD, TERMS>(a, valid, (int64_t)(sq.row0 + i) * a.q_row + (int64_t)(kvh * grps + g) * a.q_head, grp, q[mt]);
+            if (i >= n_rows) seen[mt] = Kv8Seen{0, 0, 0};
             m_run[mt] = -INFINITY, l_run[mt] = 0.f;
 #pragma unroll
             for (int d = 0; d < ND; d++) o[mt][d] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -361,13 +443,16 @@ __global__ __launch_bounds__(256, MT == 1 ? 2 : 1) void kv8_attn_stream_kernel(K
 #pragma unroll
             for (int e = 0; e < 8; e++) vs[e] *= inv;
             Half8 ph[MT][TERMS];
+            float ks[8];
+#pragma unroll
+            for (int e = 0; e < 8; e++) ks[e] = r.ks[e / 4].v[e % 4] * qf;
 #pragma unroll
             for (int mt = 0; mt < MT; mt++) {
                 float x[8], mx = -INFINITY;
                 bool vis[8];
 #pragma unroll
                 for (int e = 0; e < 8; e++) {
-                    x[e] = s[mt][e / 4][e % 4] * r.ks[e / 4].v[e % 4] * qf[mt];
+                    x[e] = s[mt][e / 4][e % 4] * ks[e];
                     if (MASKED) {
                         const int tok = t0 + 16 * (e / 4) + 4 * grp + e % 4;
                         vis[e] = tok < seen[mt].hi && (tok >= seen[mt].lo || tok < a.sinks);
@@ -464,7 +549,8 @@ __global__ __launch_bounds__(256, MT == 1 ? 2 : 1) void kv8_attn_stream_kernel(K
                         L += sL[w][row] * f;
                     }
                     const int i = (int)(m / grps), h = kvh * grps + (int)(m % grps), r = sq.row0 + i;
-                    if (tl.T <= per) { // one split: this is the result
+                    if (i >= n_rows) kv8_store_out(a, r, h, HD, d, 0.f); // an unused slot of the path
+                    else if (tl.T <= per) { // one split: this is the result
                         // (nothing seen: L is 0.  A sum that is not a number stays one.)
                         kv8_store_out(a, r, h, HD, d, L == 0.f ? 0.f : O / L);
                         if (a.lse && d == 0) a.lse[(int64_t)r * a.n_heads + h] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
@@ -477,6 +563,285 @@ __global__ __launch_bounds__(256, MT == 1 ? 2 : 1) void kv8_attn_stream_kernel(K
             }
         }
         __syncthreads();
+    }
+}
+
+// ---------------------------------------------------------------- many rows: tiles shared through LDS
+// Block: 4 waves of MT * 16 product rows each, one (sequence, cache head), one share of the tiles.  Each 32-token tile of codes is
+// widened once per block, into LDS and in the order the operands are read in (fragments of 64 x 16 bytes, so writes and reads are
+// linear), two waves doing K and two V; the next tile's codes are in flight meanwhile.  One barrier per tile.
+// The softmax's maximum follows lazily: it moves only where a score exceeds it by more than 2^K8_LAZY, so that a score costs one
+// fused multiply-add (its scale and the maximum) and one exponential.  E (see above) is known before the first tile: the block
+// looks at the V scales of its tiles once, which is 1/64 of their bytes.
+// Bound: the vector unit (per score a multiply-add, half a maximum, an exponential, a sum, a product and half a conversion, besides
+// the widening) and the matrix unit next to it.
+#define K8_LAZY 4.0f
+#define K8_P_SHIFT_LAZY 10 // p * (vs / E) * 2^10 < 2^15
+template <int HD, int MT, int TERMS>
+__global__ __launch_bounds__(256, 2) void kv8_attn_tile_kernel(Kv8View c, Kv8Rows rw, Kv8Attn a, int S, float *part)
+{
+    constexpr int NS = HD / 32, VB = HD / 16, ND = VB, NF = 2 * NS + ND; // fragments of a tile: K's, then V's
+    constexpr int ROWS = 4 * MT * 16;
+    struct Buf {
+        uint4 frag[NF][64];
+        float ks[K8_TILE], vs[K8_TILE];
+    };
+    __shared__ Buf buf[2];
+    __shared__ float red[4];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int qi = lane & 15, grp = lane >> 4;
+    const int kvh = blockIdx.x % c.kv_heads, split = blockIdx.y, grps = a.n_heads / c.kv_heads;
+    // which sequence and which of its sets of rows: the last sets (they see most) come first
+    int j, chunk;
+    {
+        int b = blockIdx.x / c.kv_heads;
+        if (!rw.row_start) {
+            const int sets = (int)(((int64_t)rw.rows * grps + ROWS - 1) / ROWS);
+            j = b % rw.n, chunk = sets - 1 - b / rw.n;
+        } else { // sets of every sequence, counted by the lanes
+            int found = -1, left = b;
+            for (int j0 = 0; j0 < rw.n && found < 0; j0 += 64) {
+                const int jj = j0 + lane;
+                const int n = jj < rw.n ? rw.row_start[jj + 1] - rw.row_start[jj] : 0;
+                const int sets = n > 0 ? (int)(((int64_t)n * grps + ROWS - 1) / ROWS) : 0;
+                int upto = sets; // of the lanes up to this one
+                for (int o = 1; o < 64; o <<= 1) {
+                    const int v = __shfl_up(upto, o, 64);
+                    if (lane >= o) upto += v;
+                }
+                const uint64_t behind = __ballot(upto > left);
+                if (behind) {
+                    const int l = __ffsll((unsigned long long)behind) - 1;
+                    found = j0 + l;
+                    left = __shfl(upto, l, 64) - 1 - left; // (counted from the sequence's end)
+                } else left -= __shfl(upto, 63, 64);
+            }
+            if (found < 0) return;
+            j = __builtin_amdgcn_readfirstlane(found), chunk = __builtin_amdgcn_readfirstlane(left);
+        }
+    }
+    const Kv8Seq sq = kv8_seq(c, rw, j);
+    if (sq.b < 0 && c.status && threadIdx.x == 0) atomicOr(c.status, 4);
+    const int n_rows = sq.b < 0 ? 0 : sq.n_rows;
+    const int64_t all = (int64_t)(rw.path ? rw.rows : n_rows) * grps, m_blk = (int64_t)chunk * ROWS, m0 = m_blk + wave * (MT * 16);
+    if (m_blk >= all) return;
+    const int cap = sq.b < 0 ? 0 : c.cap[sq.b];
+    const int64_t base = (int64_t)kvh * c.tokens + (sq.b < 0 ? 0 : c.off[sq.b]);
+    const int8_t *K = c.k + base * HD, *V = c.v + base * HD;
+    const float *KS = c.ks + base, *VS = c.vs + base;
+    const int i_first = (int)(m_blk / grps), i_last = (int)min((int64_t)n_rows - 1, (m_blk + ROWS - 1) / grps);
+    Kv8Tiles tl = {};
+    if (i_first < n_rows) tl = kv8_tiles(a, sq.len, i_first, i_last, cap);
+    const int per = kv8_per_split(tl.T, S), t_begin = split * per, t_end = min(tl.T, t_begin + per);
+    if (split > 0 && t_begin >= tl.T) return;
+    // what the wave's rows see
+    const int w_first = (int)(m0 / grps), w_last = (int)min((int64_t)n_rows - 1, (m0 + MT * 16 - 1) / grps);
+    Kv8Tiles wt = {};
+    if (w_first < n_rows) wt = kv8_tiles(a, sq.len, w_first, w_last, cap);
+    auto block_max = [&](float v) {
+        v = wave_max(v);
+        __syncthreads();
+        if (lane == 0) red[wave] = v;
+        __syncthreads();
+        return fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    };
+    f16x8 q[MT][TERMS][NS];
+    const float qf = load_queries<HD, MT, TERMS>(a, sq, n_rows, kvh, grps, m0, q, block_max);
+    float m_run[MT], l_run[MT];
+    Kv8Seen seen[MT];
+    f32x4 o[MT][ND];
+#pragma unroll
+    for (int mt = 0; mt < MT; mt++) {
+        const int i = (int)((m0 + 16 * mt + qi) / grps);
+        seen[mt] = kv8_seen(a, sq.len, i, cap);
+        if (i >= n_rows) seen[mt] = Kv8Seen{0, 0, 0};
+        m_run[mt] = -INFINITY, l_run[mt] = 0.f;
+#pragma unroll
+        for (int d = 0; d < ND; d++) o[mt][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    auto any_sees = [&](int tok) { return tok < tl.hi_max && (tok >= tl.lo_min || tok < a.sinks); };
+    float big = 0.f;
+    for (int u = t_begin * K8_TILE + threadIdx.x; u < t_end * K8_TILE; u += 256) {
+        const int tok = tl.token0(u / K8_TILE) + u % K8_TILE;
+        if (any_sees(tok)) big = fmaxf(big, VS[tok]);
+    }
+    const float E = fmaxf(KV8_SCALE_MIN, __uint_as_float(min(__float_as_uint(block_max(big)), 0x7e000000u) & 0x7f800000u));
+    const float inv_E = __uint_as_float(0x7f000000u + (K8_P_SHIFT_LAZY << 23) - __float_as_uint(E));
+    const int last_tok = max(0, tl.hi_max - 1);
+    // staging: waves 0 and 1 take 16 tokens of K each, waves 2 and 3 half of V's bytes each
+    uint4 sk[HD / 64];
+    uint32_t sv[8];
+    float ss = 0.f;
+    auto fetch = [&](int t) {
+        const int t0 = tl.token0(t);
+        const bool whole = t0 + K8_TILE <= tl.hi_max;
+        if (wave < 2) {
+            const int tok = min(16 * wave + qi, whole ? K8_TILE - 1 : last_tok - t0);
+#pragma unroll
+            for (int p = 0; p < HD / 64; p++) sk[p] = *(const uint4 *)(K + (int64_t)t0 * HD + (tok * HD + 64 * p + 16 * grp));
+        } else {
+            const int8_t *vt = V + (int64_t)t0 * HD + (VB * qi + (HD == 128 ? 4 * (wave - 2) : 0));
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                int tok = 16 * (e / 4) + 4 * grp + e % 4;
+                if (!whole) tok = min(tok, last_tok - t0);
+                sv[e] = *(const uint32_t *)(vt + tok * HD);
+            }
+        }
+        if ((wave & 1) == 0 && lane < K8_TILE) {
+            const int tok = t0 + lane;
+            ss = (wave ? VS : KS)[min(tok, last_tok)];
+            if (wave && !any_sees(tok)) ss = 0.f;
+        }
+    };
+    auto stage = [&](Buf &b) {
+        if (wave < 2) {
+#pragma unroll
+            for (int p = 0; p < HD / 64; p++) {
+                *(f16x8 *)&b.frag[wave * NS + 2 * p][lane] = codes_to_half(sk[p].x, sk[p].y);
+                *(f16x8 *)&b.frag[wave * NS + 2 * p + 1][lane] = codes_to_half(sk[p].z, sk[p].w);
+            }
+        } else {
+            Half8 f[4];
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const uint32_t a0 = sv[2 * e] ^ 0x80808080u, a1 = sv[2 * e + 1] ^ 0x80808080u;
+                if (HD == 128 || wave == 2) f[0].h[e] = pair_to_half<0>(a0, a1), f[1].h[e] = pair_to_half<1>(a0, a1);
+                if (HD == 128 || wave == 3) f[2].h[e] = pair_to_half<2>(a0, a1), f[3].h[e] = pair_to_half<3>(a0, a1);
+            }
+            uint4(*v)[64] = b.frag + 2 * NS + (HD == 128 ? 4 * (wave - 2) : 0);
+            if (HD == 128 || wave == 2) *(f16x8 *)&v[0][lane] = f[0].v, *(f16x8 *)&v[1][lane] = f[1].v;
+            if (HD == 128 || wave == 3) *(f16x8 *)&v[2][lane] = f[2].v, *(f16x8 *)&v[3][lane] = f[3].v;
+        }
+        if ((wave & 1) == 0 && lane < K8_TILE) (wave ? b.vs : b.ks)[lane] = ss * (wave ? inv_E : qf);
+    };
+    auto consume = [&](int t, const Buf &b, auto masked) {
+        constexpr bool MASKED = decltype(masked)::value;
+        const int t0 = tl.token0(t);
+        f32x4 s[MT][2];
+#pragma unroll
+        for (int mt = 0; mt < MT; mt++) s[mt][0] = s[mt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int p = 0; p < NS; p++)
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                const f16x8 k = *(const f16x8 *)&b.frag[h * NS + p][lane];
+#pragma unroll
+                for (int mt = 0; mt < MT; mt++)
+#pragma unroll
+                    for (int w = 0; w < TERMS; w++) s[mt][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[mt][w][p], s[mt][h], 0, 0, 0);
+            }
+        f32x4 ks[2], vs[2];
+#pragma unroll
+        for (int h = 0; h < 2; h++) ks[h] = *(const f32x4 *)&b.ks[16 * h + 4 * grp], vs[h] = *(const f32x4 *)&b.vs[16 * h + 4 * grp];
+        Half8 ph[MT][TERMS];
+#pragma unroll
+        for (int mt = 0; mt < MT; mt++) {
+            float y[8], mx = -INFINITY;
+            bool vis[8];
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                y[e] = fmaf(s[mt][e / 4][e % 4], ks[e / 4][e % 4], -m_run[mt]);
+                if (MASKED) {
+                    const int tok = t0 + 16 * (e / 4) + 4 * grp + e % 4;
+                    vis[e] = tok < seen[mt].hi && (tok >= seen[mt].lo || tok < a.sinks);
+                    y[e] = vis[e] ? y[e] : -INFINITY;
+                }
+                mx = fmaxf(mx, y[e]);
+            }
+            if (__any(mx > K8_LAZY)) { // (from the start, where m_run is -infinity, too)
+                asm volatile("" ::: "memory");
+                mx = -INFINITY;
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    y[e] = s[mt][e / 4][e % 4] * ks[e / 4][e % 4];
+                    if (MASKED) y[e] = vis[e] ? y[e] : -INFINITY;
+                    mx = fmaxf(mx, y[e]);
+                }
+                const float m_new = fmaxf(m_run[mt], rows4_max(mx)), ref = m_new == -INFINITY ? 0.f : m_new;
+                const float corr = __builtin_amdgcn_exp2f(m_run[mt] - ref);
+                m_run[mt] = m_new;
+                l_run[mt] *= corr;
+#pragma unroll
+                for (int d = 0; d < ND; d++) o[mt][d] *= corr;
+#pragma unroll
+                for (int e = 0; e < 8; e++) y[e] -= ref;
+            }
+            float sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                float p[2];
+#pragma unroll
+                for (int f = 0; f < 2; f++) {
+                    p[f] = __builtin_amdgcn_exp2f(y[e + f]);
+                    sum += p[f];
+                    p[f] *= vs[e / 4][e % 4 + f];
+                    if (MASKED) p[f] = vis[e + f] ? p[f] : 0.f;
+                }
+                ph[mt][0].h[e / 2] = half2_of(p[0], p[1]);
+                if constexpr (TERMS == 2)
+                    ph[mt][1].h[e / 2] = half2_of(p[0] - (float)ph[mt][0].h[e / 2][0], p[1] - (float)ph[mt][0].h[e / 2][1]);
+            }
+            l_run[mt] += sum;
+        }
+#pragma unroll
+        for (int d = 0; d < ND; d++) {
+            const f16x8 v = *(const f16x8 *)&b.frag[2 * NS + d][lane];
+#pragma unroll
+            for (int mt = 0; mt < MT; mt++)
+#pragma unroll
+                for (int w = 0; w < TERMS; w++) o[mt][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, ph[mt][w].v, o[mt][d], 0, 0, 0);
+        }
+    };
+    if (t_begin < t_end) {
+        fetch(t_begin);
+        stage(buf[0]);
+        if (t_begin + 1 < t_end) fetch(t_begin + 1);
+        for (int t = t_begin; t < t_end; t++) {
+            Buf &now = buf[(t - t_begin) & 1], &next = buf[(t - t_begin + 1) & 1];
+            __syncthreads(); // `now` is complete, and nobody reads `next` any more
+            if (t + 1 < t_end) stage(next);
+            if (t + 2 < t_end) fetch(t + 2);
+            const int t0 = tl.token0(t);
+            if (t0 < wt.hi_max && (t0 + K8_TILE > wt.lo_min || t0 < a.sinks)) { // (uniform over the wave) else its rows see nothing of it
+                if (t0 + K8_TILE <= wt.hi_min && (t0 >= wt.lo_max || t0 + K8_TILE <= a.sinks)) consume(t, now, std::false_type{});
+                else consume(t, now, std::true_type{});
+            }
+        }
+    }
+    // lane (qi, grp) holds dimensions VB (4 grp + r) .. + VB of its row in o[..][r]
+    const bool wide = kv8_wide(a.out, a.o_row, a.o_head, a.dtype);
+    const float unit = E * (K8_P_SHIFT_LAZY == 10 ? 0.5f : 0.f); // 2^(9 - 10)
+#pragma unroll
+    for (int mt = 0; mt < MT; mt++) {
+        const float l = rows4_sum(l_run[mt]);
+        const int64_t m = m0 + 16 * mt + qi;
+        if (m >= all) continue;
+        const int i = (int)(m / grps), h = kvh * grps + (int)(m % grps), r = sq.row0 + i;
+        if (i >= n_rows) { // an unused slot of the path
+#pragma unroll
+            for (int k = 0; k < 4; k++) kv8_store_run<VB>(a, wide, r, h, HD, VB * (4 * grp + k), {});
+            continue;
+        }
+        const bool done = tl.T <= per;
+        const float f = done ? (l == 0.f ? 0.f : unit / l) : unit;
+        float *p = part + (((int64_t)r * a.n_heads + h) * S + split) * (HD + 4);
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            float v[VB];
+#pragma unroll
+            for (int d = 0; d < VB; d++) v[d] = o[mt][d][k] * f;
+            const int d0 = VB * (4 * grp + k);
+            if (done) kv8_store_run<VB>(a, wide, r, h, HD, d0, v);
+            else {
+#pragma unroll
+                for (int d = 0; d < VB; d += 4) *(float4 *)(p + 4 + d0 + d) = make_float4(v[d], v[d + 1], v[d + 2], v[d + 3]);
+            }
+        }
+        if (grp == 0) {
+            if (!done) p[0] = m_run[mt], p[1] = l;
+            else if (a.lse) a.lse[(int64_t)r * a.n_heads + h] = l == 0.f ? -INFINITY : (m_run[mt] + log2f(l)) * 0.69314718055994531f;
+        }
     }
 }
 
@@ -509,24 +874,30 @@ __global__ __launch_bounds__(HD) void kv8_attn_join_kernel(Kv8View c, Kv8Rows rw
 }
 
 // ---------------------------------------------------------------- which kernel, how many blocks
+enum Kv8Kernel { KV8_PLAIN, KV8_STREAM, KV8_TILES };
 struct Kv8Plan {
-    bool stream;
-    int mt, chunks, splits;
+    int kernel, mt, set_rows, splits; // 16-row sets of a wave; product rows of a block
+    int64_t blocks;                   // per cache head and split
 };
 static Kv8Plan kv8_plan(const Kv8View &c, const Kv8Rows &rw, const Kv8Attn &a, int64_t ws_bytes)
 {
-    Kv8Plan p = {};
+    Kv8Plan p = {KV8_PLAIN, 0, 0, 1, 0};
     if ((g_force_generic & 2) || (c.hd != 64 && c.hd != 128)) return p;
-    p.stream = true;
-    const int64_t max_rows = a.max_rows > 0 ? std::min(a.max_rows, a.total_rows) : a.total_rows;
-    const int64_t R = max_rows * (a.n_heads / c.kv_heads); // rows of the products
-    p.mt = R <= 16 ? 1 : 2;
-    p.chunks = (int)std::min<int64_t>((R + 16 * p.mt - 1) / (16 * p.mt), 4096);
-    // splits: about four blocks for each of the 256 compute units, each with K8_MIN_TILES tiles at least
-    const int64_t blocks = (int64_t)rw.n * c.kv_heads * p.chunks;
+    const int64_t max_rows = a.max_rows > 0 ? std::min(a.max_rows, a.total_rows) : a.total_rows, grps = a.n_heads / c.kv_heads;
+    const int64_t R = max_rows * grps; // product rows of a sequence
+    int64_t goal; // blocks wanted on the chip
+    if (R <= 32) {
+        p.kernel = KV8_STREAM, p.mt = R <= 16 ? 1 : 2, p.set_rows = 16 * p.mt;
+        p.blocks = rw.n * ((R + p.set_rows - 1) / p.set_rows);
+        goal = 1024;
+    } else {
+        p.kernel = KV8_TILES, p.mt = 2, p.set_rows = 64 * p.mt;
+        p.blocks = rw.row_start ? a.total_rows * grps / p.set_rows + rw.n : rw.n * ((R + p.set_rows - 1) / p.set_rows);
+        goal = 512;
+    }
     const int64_t tokens = a.window ? std::min<int64_t>((int64_t)a.window + a.sinks + max_rows, (int64_t)a.max_len + max_rows) : (int64_t)a.max_len + max_rows;
-    const int64_t tiles = (tokens + K8_TILE - 1) / K8_TILE;
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(64, (tiles + K8_MIN_TILES - 1) / K8_MIN_TILES), (1024 + blocks - 1) / blocks));
+    const int64_t tiles = (tokens + K8_TILE - 1) / K8_TILE, blocks = p.blocks * c.kv_heads;
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(64, (tiles + K8_MIN_TILES - 1) / K8_MIN_TILES), (goal + blocks - 1) / blocks));
     const int64_t one = (int64_t)a.total_rows * a.n_heads * (c.hd + 4) * sizeof(float);
     if (ws_bytes >= 0 && p.splits > 1) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(p.splits, ws_bytes / one));
     return p;
@@ -535,31 +906,38 @@ static Kv8Plan kv8_plan(const Kv8View &c, const Kv8Rows &rw, const Kv8Attn &a, i
 int64_t kv8_attn_workspace(const Kv8View &c, const Kv8Rows &rw, const Kv8Attn &a)
 {
     const Kv8Plan p = kv8_plan(c, rw, a, -1);
-    return p.stream && p.splits > 1 ? (int64_t)a.total_rows * a.n_heads * (c.hd + 4) * sizeof(float) * p.splits : 0;
+    return p.splits > 1 ? (int64_t)a.total_rows * a.n_heads * (c.hd + 4) * sizeof(float) * p.splits : 0;
 }
 
 template <int HD>
-static void stream_launch(hipStream_t s, const Kv8Plan &p, const Kv8View &c, const Kv8Rows &rw, const Kv8Attn &a, float *part)
+static hipError_t mfma_launch(hipStream_t s, const Kv8Plan &p, const Kv8View &c, const Kv8Rows &rw, const Kv8Attn &a, float *part)
 {
-    const dim3 grid((unsigned)((int64_t)rw.n * c.kv_heads * p.chunks), p.splits);
-#define GO(MT, T) hipLaunchKernelGGL((kv8_attn_stream_kernel<HD, MT, T>), grid, dim3(256), 0, s, c, rw, a, p.chunks, p.splits, part)
-    if (a.dtype == SD_BF16) {
-        if (p.mt == 1) GO(1, 1);
-        else GO(2, 1);
+    if (p.blocks * c.kv_heads > 0x7fffffff / 256) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)(p.blocks * c.kv_heads), p.splits);
+#define STREAM(MT, T) hipLaunchKernelGGL((kv8_attn_stream_kernel<HD, MT, T>), grid, dim3(256), 0, s, c, rw, a, (int)(p.blocks / rw.n), p.splits, part)
+#define TILES(T) hipLaunchKernelGGL((kv8_attn_tile_kernel<HD, 2, T>), grid, dim3(256), 0, s, c, rw, a, p.splits, part)
+    const bool bf16 = a.dtype == SD_BF16;
+    if (p.kernel == KV8_TILES) {
+        if (bf16) TILES(1);
+        else TILES(2);
+    } else if (p.mt == 1) {
+        if (bf16) STREAM(1, 1);
+        else STREAM(1, 2);
     } else {
-        if (p.mt == 1) GO(1, 2);
-        else GO(2, 2);
+        if (bf16) STREAM(2, 1);
+        else STREAM(2, 2);
     }
-#undef GO
+#undef STREAM
+#undef TILES
     if (p.splits > 1)
-        hipLaunchKernelGGL(kv8_attn_join_kernel<HD>, dim3(a.total_rows, a.n_heads), dim3(HD), 0, s, c, rw, a, 16 * p.mt, p.splits, part);
+        hipLaunchKernelGGL(kv8_attn_join_kernel<HD>, dim3(a.total_rows, a.n_heads), dim3(HD), 0, s, c, rw, a, p.set_rows, p.splits, part);
+    return hipGetLastError();
 }
 
 hipError_t launch_kv8_attn(hipStream_t s, const Kv8View &c, const Kv8Rows &rw, const Kv8Attn &a, void *ws, int64_t ws_bytes)
 {
     const Kv8Plan p = kv8_plan(c, rw, a, ws_bytes);
-    if (!p.stream) hipLaunchKernelGGL(kv8_attn_generic_kernel, dim3(a.total_rows, a.n_heads), dim3(256), 0, s, c, rw, a);
-    else if (c.hd == 64) stream_launch<64>(s, p, c, rw, a, (float *)ws);
-    else stream_launch<128>(s, p, c, rw, a, (float *)ws);
+    if (p.kernel != KV8_PLAIN) return c.hd == 64 ? mfma_launch<64>(s, p, c, rw, a, (float *)ws) : mfma_launch<128>(s, p, c, rw, a, (float *)ws);
+    hipLaunchKernelGGL(kv8_attn_generic_kernel, dim3(a.total_rows, a.n_heads), dim3(256), 0, s, c, rw, a);
     return hipGetLastError();
 }

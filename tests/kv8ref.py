@@ -67,8 +67,8 @@ def attend(cache, q, parts, scale, causal=True, window=0, sinks=0):
       ds = scale * (2^-22 max|q| sum|k| + (dim + 8) 2^-24 sum|q k|) + 2^-22 |s|.
     A probability is off by its exponent's ds and by the exponential (2^-22); two terms add 2^-22, one term (bf16 rows) 2^-11; sums
     over n tokens in 32 bits n 2^-24.  Numerator and denominator both carry it: twice, against sum p|v|.  A bf16 result adds 2^-8.
-    Below all that: probabilities enter the products as halves of p * (vs / E) * 2^14 with E a power of two not above the largest
-    scale seen, whose smallest steps are 2^-24, so each token's share of an element may be off by 2^-25 2^-14 E |code|, against a
+    Below all that: probabilities enter the products as halves of p * (vs / E) * 2^10 or more with E a power of two not above the
+    largest scale seen, whose smallest steps are 2^-24, so each token's share of an element may be off by 2^-25 2^-10 E |code|, against a
     denominator of at least 1 (and an exponential below 2^-126 is 0, which is less)."""
     heads, dim = q.shape[1:]
     grp = heads // cache.k.shape[0]
@@ -94,7 +94,7 @@ def attend(cache, q, parts, scale, causal=True, window=0, sinks=0):
                 rel = ds + 2.0 ** -21 + len(see) * 2.0 ** -24
                 o = cache.off[b]
                 codes, vs = cache.v[h // grp, o:o + cache.cap[b]][see].double(), cache.vs[h // grp, o:o + cache.cap[b]][see]
-                floor = 2.0 ** -39 * vs.max().double() * codes.abs().sum(0)
+                floor = 2.0 ** -35 * vs.max().double() * codes.abs().sum(0)
                 b_out[r, h] = floor + 2 * (rel + p16) * (p @ vv.abs()) + (2.0 ** -8 if q.dtype == torch.bfloat16 else 2.0 ** -23) * out[r, h].abs()
                 b_lse[r, h] = rel + 2.0 ** -22 * lse[r, h].abs()
     return out, lse, b_out, b_lse
