@@ -578,7 +578,7 @@ __global__ __launch_bounds__(256, MT == 1 ? 2 : 1) void kv8_attn_stream_kernel(K
 #define K8_LAZY 4.0f
 #define K8_P_SHIFT_LAZY 10 // p * (vs / E) * 2^10 < 2^15
 template <int HD, int MT, int TERMS>
-__global__ __launch_bounds__(256, 2) void kv8_attn_tile_kernel(Kv8View c, Kv8Rows rw, Kv8Attn a, int S, float *part)
+__global__ __launch_bounds__(256, 3) void kv8_attn_tile_kernel(Kv8View c, Kv8Rows rw, Kv8Attn a, int S, float *part)
 {
     constexpr int NS = HD / 32, VB = HD / 16, ND = VB, NF = 2 * NS + ND; // fragments of a tile: K's, then V's
     constexpr int ROWS = 4 * MT * 16;
@@ -669,24 +669,29 @@ __global__ __launch_bounds__(256, 2) void kv8_attn_tile_kernel(Kv8View c, Kv8Row
     const float inv_E = __uint_as_float(0x7f000000u + (K8_P_SHIFT_LAZY << 23) - __float_as_uint(E));
     const int last_tok = max(0, tl.hi_max - 1);
     // staging: waves 0 and 1 take 16 tokens of K each, waves 2 and 3 half of V's bytes each
-    uint4 sk[HD / 64];
-    uint32_t sv[8];
+    uint32_t st[8]; // K: words of HD / 64 pieces; V: a word of each of eight tokens
     float ss = 0.f;
+    // (byte offsets inside a tile)
+    const uint32_t stage_at = wave < 2 ? (16 * wave + qi) * HD + 16 * grp : 4 * grp * HD + VB * qi + (HD == 128 ? 4 * (wave - 2) : 0);
     auto fetch = [&](int t) {
         const int t0 = tl.token0(t);
-        const bool whole = t0 + K8_TILE <= tl.hi_max;
-        if (wave < 2) {
-            const int tok = min(16 * wave + qi, whole ? K8_TILE - 1 : last_tok - t0);
+        if (t0 + K8_TILE <= tl.hi_max) {
+            const int8_t *tile = (wave < 2 ? K : V) + (int64_t)t0 * HD;
+            if (wave < 2) {
 #pragma unroll
-            for (int p = 0; p < HD / 64; p++) sk[p] = *(const uint4 *)(K + (int64_t)t0 * HD + (tok * HD + 64 * p + 16 * grp));
-        } else {
-            const int8_t *vt = V + (int64_t)t0 * HD + (VB * qi + (HD == 128 ? 4 * (wave - 2) : 0));
+                for (int p = 0; p < HD / 64; p++) *(uint4 *)&st[4 * p] = *(const uint4 *)(tile + stage_at + 64 * p);
+            } else {
 #pragma unroll
-            for (int e = 0; e < 8; e++) {
-                int tok = 16 * (e / 4) + 4 * grp + e % 4;
-                if (!whole) tok = min(tok, last_tok - t0);
-                sv[e] = *(const uint32_t *)(vt + tok * HD);
+                for (int e = 0; e < 8; e++) st[e] = *(const uint32_t *)(tile + stage_at + (e < 4 ? e : 12 + e) * HD);
             }
+        } else if (wave < 2) { // tokens behind the last one any row sees repeat that one
+#pragma unroll
+            for (int p = 0; p < HD / 64; p++)
+                *(uint4 *)&st[4 * p] = *(const uint4 *)(K + (int64_t)min(t0 + 16 * wave + qi, last_tok) * HD + 64 * p + 16 * grp);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+                st[e] = *(const uint32_t *)(V + (int64_t)min(t0 + 16 * (e / 4) + 4 * grp + e % 4, last_tok) * HD + VB * qi + (HD == 128 ? 4 * (wave - 2) : 0));
         }
         if ((wave & 1) == 0 && lane < K8_TILE) {
             const int tok = t0 + lane;
@@ -698,14 +703,14 @@ __global__ __launch_bounds__(256, 2) void kv8_attn_tile_kernel(Kv8View c, Kv8Row
         if (wave < 2) {
 #pragma unroll
             for (int p = 0; p < HD / 64; p++) {
-                *(f16x8 *)&b.frag[wave * NS + 2 * p][lane] = codes_to_half(sk[p].x, sk[p].y);
-                *(f16x8 *)&b.frag[wave * NS + 2 * p + 1][lane] = codes_to_half(sk[p].z, sk[p].w);
+                *(f16x8 *)&b.frag[wave * NS + 2 * p][lane] = codes_to_half(st[4 * p], st[4 * p + 1]);
+                *(f16x8 *)&b.frag[wave * NS + 2 * p + 1][lane] = codes_to_half(st[4 * p + 2], st[4 * p + 3]);
             }
         } else {
             Half8 f[4];
 #pragma unroll
             for (int e = 0; e < 4; e++) {
-                const uint32_t a0 = sv[2 * e] ^ 0x80808080u, a1 = sv[2 * e + 1] ^ 0x80808080u;
+                const uint32_t a0 = st[2 * e] ^ 0x80808080u, a1 = st[2 * e + 1] ^ 0x80808080u;
                 if (HD == 128 || wave == 2) f[0].h[e] = pair_to_half<0>(a0, a1), f[1].h[e] = pair_to_half<1>(a0, a1);
                 if (HD == 128 || wave == 3) f[2].h[e] = pair_to_half<2>(a0, a1), f[3].h[e] = pair_to_half<3>(a0, a1);
             }
@@ -731,6 +736,7 @@ __global__ __launch_bounds__(256, 2) void kv8_attn_tile_kernel(Kv8View c, Kv8Row
 #pragma unroll
                     for (int w = 0; w < TERMS; w++) s[mt][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[mt][w][p], s[mt][h], 0, 0, 0);
             }
+        __builtin_amdgcn_sched_barrier(0);
         f32x4 ks[2], vs[2];
 #pragma unroll
         for (int h = 0; h < 2; h++) ks[h] = *(const f32x4 *)&b.ks[16 * h + 4 * grp], vs[h] = *(const f32x4 *)&b.vs[16 * h + 4 * grp];
@@ -739,12 +745,13 @@ __global__ __launch_bounds__(256, 2) void kv8_attn_tile_kernel(Kv8View c, Kv8Row
         for (int mt = 0; mt < MT; mt++) {
             float y[8], mx = -INFINITY;
             bool vis[8];
+            const int rel = t0 + 4 * grp, hi = seen[mt].hi - rel, lo = seen[mt].lo - rel, sk = a.sinks - rel;
 #pragma unroll
             for (int e = 0; e < 8; e++) {
                 y[e] = fmaf(s[mt][e / 4][e % 4], ks[e / 4][e % 4], -m_run[mt]);
                 if (MASKED) {
-                    const int tok = t0 + 16 * (e / 4) + 4 * grp + e % 4;
-                    vis[e] = tok < seen[mt].hi && (tok >= seen[mt].lo || tok < a.sinks);
+                    const int tok = 16 * (e / 4) + e % 4;
+                    vis[e] = tok < hi && (tok >= lo || tok < sk);
                     y[e] = vis[e] ? y[e] : -INFINITY;
                 }
                 mx = fmaxf(mx, y[e]);
@@ -783,6 +790,7 @@ __global__ __launch_bounds__(256, 2) void kv8_attn_tile_kernel(Kv8View c, Kv8Row
                     ph[mt][1].h[e / 2] = half2_of(p[0] - (float)ph[mt][0].h[e / 2][0], p[1] - (float)ph[mt][0].h[e / 2][1]);
             }
             l_run[mt] += sum;
+            __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
         for (int d = 0; d < ND; d++) {
@@ -793,21 +801,33 @@ __global__ __launch_bounds__(256, 2) void kv8_attn_tile_kernel(Kv8View c, Kv8Row
                 for (int w = 0; w < TERMS; w++) o[mt][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, ph[mt][w].v, o[mt][d], 0, 0, 0);
         }
     };
-    if (t_begin < t_end) {
-        fetch(t_begin);
+    // Tiles that every row of the block sees whole lie together, [f0, f1): the others come first (the order does not matter to the sums),
+    // so that each of the two loops is one body.
+    int f0 = tl.n_sink + (tl.lo_max + K8_TILE - 1) / K8_TILE - tl.w0;
+    int f1 = tl.n_sink + max(0, tl.hi_min / K8_TILE - tl.w0);
+    f0 = min(max(f0, t_begin), t_end), f1 = max(f0, min(f1, t_end));
+    const int n_left = f0 - t_begin, n_edge = n_left + (t_end - f1), n = t_end - t_begin;
+    auto tile_at = [&](int u) { return u < n_left ? t_begin + u : u < n_edge ? f1 + (u - n_left) : f0 + (u - n_edge); };
+    if (n > 0) {
+        fetch(tile_at(0));
         stage(buf[0]);
-        if (t_begin + 1 < t_end) fetch(t_begin + 1);
-        for (int t = t_begin; t < t_end; t++) {
-            Buf &now = buf[(t - t_begin) & 1], &next = buf[(t - t_begin + 1) & 1];
+        if (n > 1) fetch(tile_at(1));
+        auto turn = [&](int u) { // -> this turn's tile, staged
+            Buf &now = buf[u & 1], &next = buf[(u + 1) & 1];
             __syncthreads(); // `now` is complete, and nobody reads `next` any more
-            if (t + 1 < t_end) stage(next);
-            if (t + 2 < t_end) fetch(t + 2);
-            const int t0 = tl.token0(t);
-            if (t0 < wt.hi_max && (t0 + K8_TILE > wt.lo_min || t0 < a.sinks)) { // (uniform over the wave) else its rows see nothing of it
-                if (t0 + K8_TILE <= wt.hi_min && (t0 >= wt.lo_max || t0 + K8_TILE <= a.sinks)) consume(t, now, std::false_type{});
-                else consume(t, now, std::true_type{});
-            }
+            if (u + 1 < n) stage(next);
+            __builtin_amdgcn_sched_barrier(0);
+            if (u + 2 < n) fetch(tile_at(u + 2));
+            __builtin_amdgcn_sched_barrier(0);
+            return &now;
+        };
+        int u = 0;
+        for (; u < n_edge; u++) {
+            const Buf *b = turn(u);
+            const int t = tile_at(u), t0 = tl.token0(t);
+            if (t0 < wt.hi_max && (t0 + K8_TILE > wt.lo_min || t0 < a.sinks)) consume(t, *b, std::true_type{}); // (else the wave's rows see nothing of it)
         }
+        for (; u < n; u++) consume(tile_at(u), *turn(u), std::false_type{});
     }
     // lane (qi, grp) holds dimensions VB (4 grp + r) .. + VB of its row in o[..][r]
     const bool wide = kv8_wide(a.out, a.o_row, a.o_head, a.dtype);
