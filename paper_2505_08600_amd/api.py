@@ -475,30 +475,34 @@ def rope_freqs(rot_dim: int, scaling: str = "plain", base: float = 10000.0, fact
     return out
 
 
+# (the calls below take a few microseconds on the GPU at their smallest: the binding asks torch for no more than it needs)
+_raw_stream, _device_now = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+
+
 def _rows3(t: torch.Tensor, name: str):
     """(pointer, row stride, head stride) of a [rows][heads][dim] tensor whose dimensions are adjacent."""
-    if not t.is_cuda or t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] > 1):
+    s = t.stride()
+    if not t.is_cuda or len(s) != 3 or (s[2] != 1 and t.shape[2] > 1):
         raise ValueError(f"{name}: a GPU tensor [rows][heads][dim] with adjacent dimensions is wanted")
-    return t.data_ptr(), t.stride(0), t.stride(1)
+    return t.data_ptr(), s[0], s[1]
 
 
-def _plain(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, n: int, like: torch.Tensor):
-    """Pointer of a contiguous tensor of at least n elements on like's device (None -> NULL)."""
+def _plain(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, n: int, dev: int):
+    """Pointer of a contiguous tensor of at least n elements on GPU dev (None -> NULL)."""
     if t is None:
         return None
-    if t.dtype != dtype or t.numel() < n or not t.is_contiguous() or t.device != like.device:
-        raise ValueError(f"{name}: a contiguous {dtype} tensor of at least {n} elements on {like.device} is wanted")
+    if t.dtype is not dtype or t.numel() < n or not t.is_contiguous() or t.get_device() != dev:
+        raise ValueError(f"{name}: a contiguous {dtype} tensor of at least {n} elements on GPU {dev} is wanted")
     return t.data_ptr()
 
 
-def _call_on(t: torch.Tensor, fn, *args) -> None:
-    """fn(*args, current stream of t's device) with that device current."""
-    dev = t.get_device()
-    if dev == torch.cuda.current_device():
-        rc = fn(*args, torch.cuda.current_stream().cuda_stream)
+def _call_on(dev: int, fn, *args) -> None:
+    """fn(*args, current stream of GPU dev) with that GPU current."""
+    if dev == _device_now():
+        rc = fn(*args, _raw_stream(dev))
     else:
         with torch.cuda.device(dev):
-            rc = fn(*args, torch.cuda.current_stream().cuda_stream)
+            rc = fn(*args, _raw_stream(dev))
     if rc != SD_OK:
         _check(rc)
 
@@ -511,12 +515,12 @@ def sd_rope(x: torch.Tensor, pos: torch.Tensor, inv_freq: torch.Tensor, out: Opt
         raise ValueError("x: float32 or bfloat16 is wanted")
     if out is None:
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    if out.shape != x.shape or out.dtype != x.dtype or out.device != x.device:
+    dev, xs, ys = x.get_device(), _rows3(x, "x"), _rows3(out, "out")
+    if out.shape != x.shape or out.dtype is not x.dtype or out.get_device() != dev:
         raise ValueError("out: a tensor like x is wanted")
     rows, heads, dim = x.shape
-    _call_on(x, lib().sd_rope, *_rows3(x, "x"), *_rows3(out, "out"), _DTYPES[x.dtype], rows, heads, dim, 2 * inv_freq.numel(),
-             _plain(pos, "pos", torch.int32, rows, x), _plain(inv_freq, "inv_freq", torch.float64, 1, x), gain, int(interleaved),
-             int(inverse))
+    _call_on(dev, lib().sd_rope, *xs, *ys, _DTYPES[x.dtype], rows, heads, dim, 2 * inv_freq.numel(),
+             _plain(pos, "pos", torch.int32, rows, dev), _plain(inv_freq, "inv_freq", torch.float64, 1, dev), gain, interleaved, inverse)
     return out
 
 
@@ -529,13 +533,13 @@ class Kv8Cache:
         if not k.is_cuda or k.dim() != 3:
             raise ValueError("k: a GPU tensor [kv_heads][tokens][dim] is wanted")
         heads, tokens, dim = k.shape
-        n, n_seq = heads * tokens, cap.numel()
-        self.k, self.n_seq, self.kv_heads, self.head_dim = k, n_seq, heads, dim
+        n, n_seq, dev = heads * tokens, cap.numel(), k.get_device()
+        self.k, self.n_seq, self.kv_heads, self.head_dim, self.dev = k, n_seq, heads, dim, dev
         self._keep = (v, k_scale, v_scale, off, cap, status)
-        self.c = _Kv8(_plain(k, "k", torch.int8, n * dim, k), _plain(v, "v", torch.int8, n * dim, k),
-                      _plain(k_scale, "k_scale", torch.float32, n, k), _plain(v_scale, "v_scale", torch.float32, n, k), tokens,
-                      heads, dim, n_seq, _plain(off, "off", torch.int64, n_seq, k), _plain(cap, "cap", torch.int32, n_seq, k),
-                      _plain(status, "status", torch.int32, 1, k))
+        self.c = _Kv8(_plain(k, "k", torch.int8, n * dim, dev), _plain(v, "v", torch.int8, n * dim, dev),
+                      _plain(k_scale, "k_scale", torch.float32, n, dev), _plain(v_scale, "v_scale", torch.float32, n, dev), tokens,
+                      heads, dim, n_seq, _plain(off, "off", torch.int64, n_seq, dev), _plain(cap, "cap", torch.int32, n_seq, dev),
+                      _plain(status, "status", torch.int32, 1, dev))
 
     @classmethod
     def empty(cls, caps: Sequence[int], kv_heads: int, head_dim: int, device="cuda") -> "Kv8Cache":
@@ -554,21 +558,20 @@ class Kv8Cache:
 
     def _rows(self, length: torch.Tensor, seq_ids: Optional[torch.Tensor], row_start: Optional[torch.Tensor]):
         n = self.n_seq if seq_ids is None else seq_ids.numel()
-        return (_plain(seq_ids, "seq_ids", torch.int32, 1, self.k), n, _plain(length, "length", torch.int32, self.n_seq, self.k),
-                _plain(row_start, "row_start", torch.int32, n + 1, self.k))
+        return (_plain(seq_ids, "seq_ids", torch.int32, 1, self.dev), n, _plain(length, "length", torch.int32, self.n_seq, self.dev),
+                _plain(row_start, "row_start", torch.int32, n + 1, self.dev))
 
 
 def _kv8_move(fn, cache: Kv8Cache, length, k, v, seq_ids, row_start) -> None:
     one = k if k is not None else v
     if one is None or one.dtype not in _DTYPES:
         raise ValueError("k, v: float32 or bfloat16 is wanted")
+    want = (one.shape[0], cache.kv_heads, cache.head_dim)
     for t in (k, v):
-        if t is not None and (t.dtype != one.dtype or t.shape[0] != one.shape[0] or t.device != cache.k.device or
-                              tuple(t.shape[1:]) != (cache.kv_heads, cache.head_dim)):
+        if t is not None and (t.dtype is not one.dtype or t.shape != want or t.get_device() != cache.dev):
             raise ValueError("k, v: tensors [rows][kv_heads][dim] of one type on the cache's device are wanted")
-    none = (None, 0, 0)
-    _call_on(cache.k, fn, C.byref(cache.c), *cache._rows(length, seq_ids, row_start), one.shape[0], _DTYPES[one.dtype],
-             *(none if k is None else _rows3(k, "k")), *(none if v is None else _rows3(v, "v")))
+    _call_on(cache.dev, fn, cache.c, *cache._rows(length, seq_ids, row_start), want[0], _DTYPES[one.dtype],
+             *((None, 0, 0) if k is None else _rows3(k, "k")), *((None, 0, 0) if v is None else _rows3(v, "v")))
 
 
 def sd_kv8_append(cache: Kv8Cache, length: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seq_ids: Optional[torch.Tensor] = None,
@@ -590,15 +593,16 @@ def sd_kv8_attend(cache: Kv8Cache, length: torch.Tensor, q: torch.Tensor, out: t
     """sd_kv8_attend: q, out [rows][heads][dim]; lse float32 [rows][heads].  max_len: the largest length (and, with row_start, max_rows
     the most rows of one sequence), as far as the caller knows them: they size launches, not results.  The workspace is the
     caching allocator's, in order with the current stream; without memory for it the call runs without one."""
-    if q.dtype not in _DTYPES or out.dtype != q.dtype or out.shape != q.shape or q.device != cache.k.device or out.device != q.device:
+    dev = cache.dev
+    if q.dtype not in _DTYPES or out.dtype is not q.dtype or out.shape != q.shape or q.get_device() != dev or out.get_device() != dev:
         raise ValueError("q, out: float32 or bfloat16 tensors of one shape on the cache's device are wanted")
     if q.dim() != 3 or q.shape[2] != cache.head_dim:
         raise ValueError("q: a tensor [rows][heads][dim] with the cache's dim is wanted")
     rows, heads, _ = q.shape
     ids, n, lens, starts = cache._rows(length, seq_ids, row_start)
     a = _Kv8Attn(ids, lens, starts, n, rows, max_rows, max_len, heads, _DTYPES[q.dtype], *_rows3(q, "q"), *_rows3(out, "out"),
-                 _plain(lse, "lse", torch.float32, rows * heads, q), scale, int(causal), window, sinks, None, 0)
-    need = lib().sd_kv8_attend_workspace(C.byref(cache.c), C.byref(a))
+                 _plain(lse, "lse", torch.float32, rows * heads, dev), scale, causal, window, sinks, None, 0)
+    need = lib().sd_kv8_attend_workspace(cache.c, a)
     if need < 0:
         _check(need)
     ws = None
@@ -608,7 +612,7 @@ def sd_kv8_attend(cache: Kv8Cache, length: torch.Tensor, q: torch.Tensor, out: t
             a.workspace, a.workspace_bytes = ws.data_ptr(), need
         except torch.OutOfMemoryError:
             pass
-    _call_on(cache.k, lib().sd_kv8_attend, C.byref(cache.c), C.byref(a))
+    _call_on(dev, lib().sd_kv8_attend, cache.c, a)
 
 
 def eq1_speedup(alpha: float, gamma: int, c: float) -> float:

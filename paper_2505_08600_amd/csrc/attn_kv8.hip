@@ -218,9 +218,25 @@ __device__ __forceinline__ Kv8Tiles kv8_tiles(const Kv8Attn &a, int len, int i0,
     t.T = t.n_sink + (t.hi_max + K8_TILE - 1) / K8_TILE - t.w0;
     return t;
 }
-// Tiles per split: an even share, and at least so many that a block has something to stream.
-#define K8_MIN_TILES 16
-__device__ __forceinline__ int kv8_per_split(int T, int S) { return max(K8_MIN_TILES, (T + S - 1) / S); }
+// The tiles [t_begin, t_end) in the order a block takes them: those that every row sees whole lie together, [f0, f1), and come last (the order
+// does not matter to the sums), so that the loops over either kind have one body each.
+struct Kv8Order {
+    int t_begin, f0, f1, n_left, n_edge, n;
+    __device__ __forceinline__ int tile(int u) const { return u < n_left ? t_begin + u : u < n_edge ? f1 + (u - n_left) : f0 + (u - n_edge); }
+};
+__device__ __forceinline__ Kv8Order kv8_order(const Kv8Tiles &tl, int t_begin, int t_end)
+{
+    Kv8Order o;
+    o.t_begin = t_begin;
+    o.f0 = min(max(tl.n_sink + (tl.lo_max + K8_TILE - 1) / K8_TILE - tl.w0, t_begin), t_end);
+    o.f1 = max(o.f0, min(tl.n_sink + tl.hi_min / K8_TILE - tl.w0, t_end));
+    o.n_left = o.f0 - t_begin, o.n_edge = o.n_left + (t_end - o.f1), o.n = max(0, t_end - t_begin);
+    return o;
+}
+
+// Tiles per split: what the launch was sized for, so that the blocks of short and long sequences do the same work - or, of a sequence
+// longer than the launch was told of, an even share.
+__device__ __forceinline__ int kv8_per_split(int T, int S, int per) { return max(per, (T + S - 1) / S); }
 
 // 16 adjacent elements of a query row
 template <int TERMS>
@@ -337,7 +353,7 @@ struct K8Regs {
 // E, a power of two above half the largest V scale so far, takes the scales' range out of the 16-bit probabilities.
 // Bound: memory; per code about 1.2 vector operations to widen it, beside one matrix instruction per 512 codes and 16 rows.
 template <int HD, int MT, int TERMS>
-__global__ __launch_bounds__(256, MT == 1 ? 2 : 1) void kv8_attn_stream_kernel(Kv8View c, Kv8Rows rw, Kv8Attn a, int n_chunks, int S, float *part)
+__global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void kv8_attn_stream_kernel(Kv8View c, Kv8Rows rw, Kv8Attn a, int n_chunks, int S, int per_want, float *part)
 {
     constexpr int NS = HD / 32, VB = HD / 16, VW = HD / 64, ND = VB;
     constexpr int DP = HD < 128 ? HD : 128; // dimensions merged at a time
@@ -359,7 +375,7 @@ __global__ __launch_bounds__(256, MT == 1 ? 2 : 1) void kv8_attn_stream_kernel(K
         const int i_first = (int)(m0 / grps), i_last = (int)min((int64_t)n_rows - 1, (m0 + MT * 16 - 1) / grps);
         Kv8Tiles tl = {};
         if (i_first < n_rows) tl = kv8_tiles(a, sq.len, i_first, i_last, cap);
-        const int per = kv8_per_split(tl.T, S), t_begin = split * per, t_end = min(tl.T, t_begin + per);
+        const int per = kv8_per_split(tl.T, S, per_want), t_begin = split * per, t_end = min(tl.T, t_begin + per);
         if (split > 0 && t_begin >= tl.T) continue;
         f16x8 q[MT][TERMS][NS];
         const float qf = load_queries<HD, MT, TERMS>(a, sq, n_rows, kvh, grps, m0, q, wave_max); // (the same for every wave: they hold the same rows)
@@ -378,17 +394,17 @@ __global__ __launch_bounds__(256, MT == 1 ? 2 : 1) void kv8_attn_stream_kernel(K
         float E = KV8_SCALE_MIN;
         const int last_tok = max(0, tl.hi_max - 1);
         const uint32_t k_lane = qi * HD + 16 * grp, v_lane = 4 * grp * HD + VB * qi; // byte offsets of the lane inside a tile
-        auto load = [&](int t, K8Regs<HD> &r) {
+        // One tile's bytes: they are asked for where the tile before it has used the registers up, K and the scales behind the score
+        // products, V behind the output products.
+        K8Regs<HD> r;
+        auto load_k = [&](int t) {
             const int t0 = tl.token0(t);
             if (t0 + K8_TILE <= tl.hi_max) { // (uniform) a whole tile: one address and constant offsets
-                const int8_t *kt = K + (int64_t)t0 * HD, *vt = V + (int64_t)t0 * HD;
+                const int8_t *kt = K + (int64_t)t0 * HD;
 #pragma unroll
                 for (int h = 0; h < 2; h++)
 #pragma unroll
                     for (int p = 0; p < HD / 64; p++) r.k[h][p] = *(const uint4 *)(kt + k_lane + (16 * h * HD + 64 * p));
-#pragma unroll
-                for (int e = 0; e < 8; e++)
-                    r.v[e] = *(const typename K8Regs<HD>::VRow *)(vt + v_lane + (e < 4 ? e : 12 + e) * HD);
 #pragma unroll
                 for (int h = 0; h < 2; h++) r.ks[h] = *(const F4 *)(KS + t0 + 16 * h + 4 * grp), r.vs[h] = *(const F4 *)(VS + t0 + 16 * h + 4 * grp);
             } else { // tokens behind the last one any row sees repeat that one
@@ -399,14 +415,25 @@ __global__ __launch_bounds__(256, MT == 1 ? 2 : 1) void kv8_attn_stream_kernel(K
 #pragma unroll
                 for (int e = 0; e < 8; e++) {
                     const int tok = min(t0 + 16 * (e / 4) + 4 * grp + e % 4, last_tok);
-                    r.v[e] = *(const typename K8Regs<HD>::VRow *)(V + (int64_t)tok * HD + VB * qi);
                     r.ks[e / 4].v[e % 4] = KS[tok], r.vs[e / 4].v[e % 4] = VS[tok];
                 }
             }
         };
-        auto consume = [&](int t, const K8Regs<HD> &r, auto masked) {
-            constexpr bool MASKED = decltype(masked)::value;
+        auto load_v = [&](int t) {
             const int t0 = tl.token0(t);
+            if (t0 + K8_TILE <= tl.hi_max) {
+                const int8_t *vt = V + (int64_t)t0 * HD;
+#pragma unroll
+                for (int e = 0; e < 8; e++) r.v[e] = *(const typename K8Regs<HD>::VRow *)(vt + v_lane + (e < 4 ? e : 12 + e) * HD);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; e++)
+                    r.v[e] = *(const typename K8Regs<HD>::VRow *)(V + (int64_t)min(t0 + 16 * (e / 4) + 4 * grp + e % 4, last_tok) * HD + VB * qi);
+            }
+        };
+        auto consume = [&](int t, int t_next, auto masked) { // t_next < 0: none
+            constexpr bool MASKED = decltype(masked)::value;
+            const int rel = tl.token0(t) + 4 * grp; // tokens are counted from the lane's first one
             f32x4 s[MT][2];
 #pragma unroll
             for (int mt = 0; mt < MT; mt++) s[mt][0] = s[mt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -423,18 +450,21 @@ __global__ __launch_bounds__(256, MT == 1 ? 2 : 1) void kv8_attn_stream_kernel(K
                             s[mt][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, q[mt][w][2 * p + 1], s[mt][h], 0, 0, 0);
                         }
                 }
-            __builtin_amdgcn_sched_barrier(0);
-            // the tile's V scales over E
-            float vs[8], big = 0.f;
+            float ks[8], vs[8], big = 0.f;
 #pragma unroll
             for (int e = 0; e < 8; e++) {
+                ks[e] = r.ks[e / 4].v[e % 4] * qf;
                 vs[e] = r.vs[e / 4].v[e % 4];
                 if (MASKED) { // scales of tokens that no row sees are not looked at
-                    const int tok = t0 + 16 * (e / 4) + 4 * grp + e % 4;
-                    if (!(tok < tl.hi_max && (tok >= tl.lo_min || tok < a.sinks))) vs[e] = 0.f;
+                    const int tok = 16 * (e / 4) + e % 4;
+                    if (!(tok < tl.hi_max - rel && (tok >= tl.lo_min - rel || tok < a.sinks - rel))) vs[e] = 0.f;
                 }
                 big = fmaxf(big, vs[e]);
             }
+            __builtin_amdgcn_sched_barrier(0);
+            if (t_next >= 0) load_k(t_next);
+            __builtin_amdgcn_sched_barrier(0);
+            // the tile's V scales over E
             big = __uint_as_float(min(__float_as_uint(rows4_max(big)), 0x7e000000u) & 0x7f800000u);
             const float E_new = fmaxf(E, big);
             const float inv = __uint_as_float(0x7f000000u + (K8_P_SHIFT << 23) - __float_as_uint(E_new));
@@ -443,19 +473,17 @@ __global__ __launch_bounds__(256, MT == 1 ? 2 : 1) void kv8_attn_stream_kernel(K
 #pragma unroll
             for (int e = 0; e < 8; e++) vs[e] *= inv;
             Half8 ph[MT][TERMS];
-            float ks[8];
-#pragma unroll
-            for (int e = 0; e < 8; e++) ks[e] = r.ks[e / 4].v[e % 4] * qf;
 #pragma unroll
             for (int mt = 0; mt < MT; mt++) {
                 float x[8], mx = -INFINITY;
                 bool vis[8];
+                const int hi = seen[mt].hi - rel, lo = seen[mt].lo - rel, sk = a.sinks - rel;
 #pragma unroll
                 for (int e = 0; e < 8; e++) {
                     x[e] = s[mt][e / 4][e % 4] * ks[e];
                     if (MASKED) {
-                        const int tok = t0 + 16 * (e / 4) + 4 * grp + e % 4;
-                        vis[e] = tok < seen[mt].hi && (tok >= seen[mt].lo || tok < a.sinks);
+                        const int tok = 16 * (e / 4) + e % 4;
+                        vis[e] = tok < hi && (tok >= lo || tok < sk);
                         x[e] = vis[e] ? x[e] : -INFINITY;
                     }
                     mx = fmaxf(mx, x[e]);
@@ -485,9 +513,9 @@ __global__ __launch_bounds__(256, MT == 1 ? 2 : 1) void kv8_attn_stream_kernel(K
 #pragma unroll
                     for (int d = 0; d < ND; d++) o[mt][d] *= corr_o;
                 }
+                __builtin_amdgcn_sched_barrier(0);
             }
             // V^T fragments, byte by byte of the words
-            __builtin_amdgcn_sched_barrier(0); // (widened early, the fragments would cost a second set of registers)
 #pragma unroll
             for (int w = 0; w < VW; w++) {
                 Half8 f[4];
@@ -506,19 +534,18 @@ __global__ __launch_bounds__(256, MT == 1 ? 2 : 1) void kv8_attn_stream_kernel(K
 #pragma unroll
                         for (int u = 0; u < TERMS; u++)
                             o[mt][4 * w + b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[b].v, ph[mt][u].v, o[mt][4 * w + b], 0, 0, 0);
-            }
-        };
-        if (t_begin + wave < t_end) {
-            K8Regs<HD> cur, next;
-            load(t_begin + wave, cur);
-            for (int t = t_begin + wave; t < t_end; t += 4) {
-                if (t + 4 < t_end) load(t + 4, next);
                 __builtin_amdgcn_sched_barrier(0);
-                const int t0 = tl.token0(t);
-                if (t0 + K8_TILE <= tl.hi_min && (t0 >= tl.lo_max || t0 + K8_TILE <= a.sinks)) consume(t, cur, std::false_type{});
-                else consume(t, cur, std::true_type{});
-                cur = next;
             }
+            if (t_next >= 0) load_v(t_next);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        const Kv8Order od = kv8_order(tl, t_begin, t_end);
+        if (wave < od.n) {
+            int u = wave;
+            load_k(od.tile(u));
+            load_v(od.tile(u));
+            for (; u < od.n_edge; u += 4) consume(od.tile(u), u + 4 < od.n ? od.tile(u + 4) : -1, std::true_type{});
+            for (; u < od.n; u += 4) consume(od.tile(u), u + 4 < od.n ? od.tile(u + 4) : -1, std::false_type{});
         }
         // the waves' parts meet: O in true units (E and the shifts undone), weighted by their maxima
         const float unit = E * 0.03125f; // 2^(9 - 14)
@@ -578,7 +605,7 @@ __global__ __launch_bounds__(256, MT == 1 ? 2 : 1) void kv8_attn_stream_kernel(K
 #define K8_LAZY 4.0f
 #define K8_P_SHIFT_LAZY 10 // p * (vs / E) * 2^10 < 2^15
 template <int HD, int MT, int TERMS>
-__global__ __launch_bounds__(256, 3) void kv8_attn_tile_kernel(Kv8View c, Kv8Rows rw, Kv8Attn a, int S, float *part)
+__global__ __launch_bounds__(256, 3) void kv8_attn_tile_kernel(Kv8View c, Kv8Rows rw, Kv8Attn a, int S, int per_want, float *part)
 {
     constexpr int NS = HD / 32, VB = HD / 16, ND = VB, NF = 2 * NS + ND; // fragments of a tile: K's, then V's
     constexpr int ROWS = 4 * MT * 16;
@@ -632,7 +659,7 @@ __global__ __launch_bounds__(256, 3) void kv8_attn_tile_kernel(Kv8View c, Kv8Row
     const int i_first = (int)(m_blk / grps), i_last = (int)min((int64_t)n_rows - 1, (m_blk + ROWS - 1) / grps);
     Kv8Tiles tl = {};
     if (i_first < n_rows) tl = kv8_tiles(a, sq.len, i_first, i_last, cap);
-    const int per = kv8_per_split(tl.T, S), t_begin = split * per, t_end = min(tl.T, t_begin + per);
+    const int per = kv8_per_split(tl.T, S, per_want), t_begin = split * per, t_end = min(tl.T, t_begin + per);
     if (split > 0 && t_begin >= tl.T) return;
     // what the wave's rows see
     const int w_first = (int)(m0 / grps), w_last = (int)min((int64_t)n_rows - 1, (m0 + MT * 16 - 1) / grps);
@@ -801,13 +828,9 @@ __global__ __launch_bounds__(256, 3) void kv8_attn_tile_kernel(Kv8View c, Kv8Row
                 for (int w = 0; w < TERMS; w++) o[mt][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, ph[mt][w].v, o[mt][d], 0, 0, 0);
         }
     };
-    // Tiles that every row of the block sees whole lie together, [f0, f1): the others come first (the order does not matter to the sums),
-    // so that each of the two loops is one body.
-    int f0 = tl.n_sink + (tl.lo_max + K8_TILE - 1) / K8_TILE - tl.w0;
-    int f1 = tl.n_sink + max(0, tl.hi_min / K8_TILE - tl.w0);
-    f0 = min(max(f0, t_begin), t_end), f1 = max(f0, min(f1, t_end));
-    const int n_left = f0 - t_begin, n_edge = n_left + (t_end - f1), n = t_end - t_begin;
-    auto tile_at = [&](int u) { return u < n_left ? t_begin + u : u < n_edge ? f1 + (u - n_left) : f0 + (u - n_edge); };
+    const Kv8Order od = kv8_order(tl, t_begin, t_end);
+    const int n = od.n;
+    auto tile_at = [&](int u) { return od.tile(u); };
     if (n > 0) {
         fetch(tile_at(0));
         stage(buf[0]);
@@ -822,7 +845,7 @@ __global__ __launch_bounds__(256, 3) void kv8_attn_tile_kernel(Kv8View c, Kv8Row
             return &now;
         };
         int u = 0;
-        for (; u < n_edge; u++) {
+        for (; u < od.n_edge; u++) {
             const Buf *b = turn(u);
             const int t = tile_at(u), t0 = tl.token0(t);
             if (t0 < wt.hi_max && (t0 + K8_TILE > wt.lo_min || t0 < a.sinks)) consume(t, *b, std::true_type{}); // (else the wave's rows see nothing of it)
@@ -867,7 +890,7 @@ __global__ __launch_bounds__(256, 3) void kv8_attn_tile_kernel(Kv8View c, Kv8Row
 
 // Joins the splits of one (row, head).
 template <int HD>
-__global__ __launch_bounds__(HD) void kv8_attn_join_kernel(Kv8View c, Kv8Rows rw, Kv8Attn a, int set_rows, int S, const float *__restrict__ part)
+__global__ __launch_bounds__(HD) void kv8_attn_join_kernel(Kv8View c, Kv8Rows rw, Kv8Attn a, int set_rows, int S, int per_want, const float *__restrict__ part)
 {
     const int r = blockIdx.x, h = blockIdx.y, d = threadIdx.x;
     const int j = kv8_owner(rw, r);
@@ -877,7 +900,7 @@ __global__ __launch_bounds__(HD) void kv8_attn_join_kernel(Kv8View c, Kv8Rows rw
     if (sq.b < 0 || i >= sq.n_rows) return;
     const int64_t m0 = ((int64_t)i * grps + h % grps) / set_rows * set_rows; // the set of rows that the row went with
     const int i_last = (int)min((int64_t)sq.n_rows - 1, (m0 + set_rows - 1) / grps);
-    const int T = kv8_tiles(a, sq.len, (int)(m0 / grps), i_last, c.cap[sq.b]).T, per = kv8_per_split(T, S), used = (T + per - 1) / per;
+    const int T = kv8_tiles(a, sq.len, (int)(m0 / grps), i_last, c.cap[sq.b]).T, per = kv8_per_split(T, S, per_want), used = (T + per - 1) / per;
     if (used <= 1) return; // the block has written the result
     const float *p = part + ((int64_t)r * a.n_heads + h) * S * (HD + 4);
     float M = -INFINITY;
@@ -894,14 +917,16 @@ __global__ __launch_bounds__(HD) void kv8_attn_join_kernel(Kv8View c, Kv8Rows rw
 }
 
 // ---------------------------------------------------------------- which kernel, how many blocks
+#define K8_MIN_TILES 16
+#define K8_MAX_SPLITS 64
 enum Kv8Kernel { KV8_PLAIN, KV8_STREAM, KV8_TILES };
 struct Kv8Plan {
-    int kernel, mt, set_rows, splits; // 16-row sets of a wave; product rows of a block
+    int kernel, mt, set_rows, splits, per; // 16-row sets of a wave; product rows of a block; splits of a context and tiles of one
     int64_t blocks;                   // per cache head and split
 };
 static Kv8Plan kv8_plan(const Kv8View &c, const Kv8Rows &rw, const Kv8Attn &a, int64_t ws_bytes)
 {
-    Kv8Plan p = {KV8_PLAIN, 0, 0, 1, 0};
+    Kv8Plan p = {KV8_PLAIN, 0, 0, 1, 0, 0};
     if ((g_force_generic & 2) || (c.hd != 64 && c.hd != 128)) return p;
     const int64_t max_rows = a.max_rows > 0 ? std::min(a.max_rows, a.total_rows) : a.total_rows, grps = a.n_heads / c.kv_heads;
     const int64_t R = max_rows * grps; // product rows of a sequence
@@ -909,7 +934,7 @@ static Kv8Plan kv8_plan(const Kv8View &c, const Kv8Rows &rw, const Kv8Attn &a, i
     if (R <= 32) {
         p.kernel = KV8_STREAM, p.mt = R <= 16 ? 1 : 2, p.set_rows = 16 * p.mt;
         p.blocks = rw.n * ((R + p.set_rows - 1) / p.set_rows);
-        goal = 1024;
+        goal = 2048;
     } else {
         p.kernel = KV8_TILES, p.mt = 2, p.set_rows = 64 * p.mt;
         p.blocks = rw.row_start ? a.total_rows * grps / p.set_rows + rw.n : rw.n * ((R + p.set_rows - 1) / p.set_rows);
@@ -917,7 +942,9 @@ static Kv8Plan kv8_plan(const Kv8View &c, const Kv8Rows &rw, const Kv8Attn &a, i
     }
     const int64_t tokens = a.window ? std::min<int64_t>((int64_t)a.window + a.sinks + max_rows, (int64_t)a.max_len + max_rows) : (int64_t)a.max_len + max_rows;
     const int64_t tiles = (tokens + K8_TILE - 1) / K8_TILE, blocks = p.blocks * c.kv_heads;
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(64, (tiles + K8_MIN_TILES - 1) / K8_MIN_TILES), (goal + blocks - 1) / blocks));
+    // a split takes K8_MIN_TILES tiles at least and the context K8_MAX_SPLITS splits at most
+    p.per = (int)std::max(std::max<int64_t>((tiles * blocks + goal - 1) / goal, (tiles + K8_MAX_SPLITS - 1) / K8_MAX_SPLITS), (int64_t)K8_MIN_TILES);
+    p.splits = (int)std::max<int64_t>(1, (tiles + p.per - 1) / p.per);
     const int64_t one = (int64_t)a.total_rows * a.n_heads * (c.hd + 4) * sizeof(float);
     if (ws_bytes >= 0 && p.splits > 1) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(p.splits, ws_bytes / one));
     return p;
@@ -934,8 +961,8 @@ static hipError_t mfma_launch(hipStream_t s, const Kv8Plan &p, const Kv8View &c,
 {
     if (p.blocks * c.kv_heads > 0x7fffffff / 256) return hipErrorInvalidValue;
     const dim3 grid((unsigned)(p.blocks * c.kv_heads), p.splits);
-#define STREAM(MT, T) hipLaunchKernelGGL((kv8_attn_stream_kernel<HD, MT, T>), grid, dim3(256), 0, s, c, rw, a, (int)(p.blocks / rw.n), p.splits, part)
-#define TILES(T) hipLaunchKernelGGL((kv8_attn_tile_kernel<HD, 2, T>), grid, dim3(256), 0, s, c, rw, a, p.splits, part)
+#define STREAM(MT, T) hipLaunchKernelGGL((kv8_attn_stream_kernel<HD, MT, T>), grid, dim3(256), 0, s, c, rw, a, (int)(p.blocks / rw.n), p.splits, p.per, part)
+#define TILES(T) hipLaunchKernelGGL((kv8_attn_tile_kernel<HD, 2, T>), grid, dim3(256), 0, s, c, rw, a, p.splits, p.per, part)
     const bool bf16 = a.dtype == SD_BF16;
     if (p.kernel == KV8_TILES) {
         if (bf16) TILES(1);
@@ -950,7 +977,7 @@ static hipError_t mfma_launch(hipStream_t s, const Kv8Plan &p, const Kv8View &c,
 #undef STREAM
 #undef TILES
     if (p.splits > 1)
-        hipLaunchKernelGGL(kv8_attn_join_kernel<HD>, dim3(a.total_rows, a.n_heads), dim3(HD), 0, s, c, rw, a, p.set_rows, p.splits, part);
+        hipLaunchKernelGGL(kv8_attn_join_kernel<HD>, dim3(a.total_rows, a.n_heads), dim3(HD), 0, s, c, rw, a, p.set_rows, p.splits, p.per, part);
     return hipGetLastError();
 }
 
