@@ -295,7 +295,7 @@ typedef struct {
     int32_t head_dim;        /* a multiple of 16 in 16..256 */
     int32_t n_seq;           /* >= 1 */
     const int64_t *off;      /* int64[n_seq], every off[b] + cap[b] <= tokens */
-    const int32_t *cap;      /* int32[n_seq] */
+    const int32_t *cap;      /* int32[n_seq]; tokens behind the first 2^30 of a sequence are not looked at */
     int32_t *status;         /* int32[1] or NULL: sticky bits, 1 = a row outside its sequence's capacity, 4 = a sequence id out of range */
 } sd_kv8;
 

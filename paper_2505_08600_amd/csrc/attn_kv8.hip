@@ -12,10 +12,10 @@ struct Kv8Seen {
 };
 __device__ __forceinline__ Kv8Seen kv8_seen(const Kv8Attn &a, int len, int i, int cap)
 {
-    const int64_t end = a.causal ? (int64_t)len + i + 1 : len;
+    const int end = a.causal ? len + i + 1 : len;
     Kv8Seen s;
-    s.hi = (int)max((int64_t)0, min(end, (int64_t)cap));
-    s.lo = a.window ? (int)min((int64_t)s.hi, max((int64_t)0, end - a.window)) : 0;
+    s.hi = max(0, min(end, cap));
+    s.lo = a.window ? min(s.hi, max(0, end - a.window)) : 0;
     s.n_first = min(a.sinks, s.lo);
     return s;
 }
@@ -72,7 +72,7 @@ __global__ __launch_bounds__(256) void kv8_attn_generic_kernel(Kv8View c, Kv8Row
             for (int d = tid; d < hd; d += 256) kv8_store_out(a, r, h, hd, d, 0.f);
         return;
     }
-    const Kv8Seen seen = kv8_seen(a, s.len, i, c.cap[s.b]);
+    const Kv8Seen seen = kv8_seen(a, s.len, i, kv8_capacity(c, s.b));
     const int n = seen.n_first + (seen.hi - seen.lo);
     const int64_t base = (int64_t)(h / (a.n_heads / c.kv_heads)) * c.tokens + c.off[s.b];
     for (int d = tid; d < hd; d += 256)
@@ -137,11 +137,10 @@ __global__ __launch_bounds__(256) void kv8_attn_generic_kernel(Kv8View c, Kv8Row
 typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
-struct __attribute__((packed, aligned(4))) F4 { // four floats at any element
-    float v[4];
-};
 
 #define K8_TILE 32
+#define K8_MIN_TILES 16  // tiles of a split at least
+#define K8_MAX_SPLITS 64 // splits of a context at most
 #define K8_P_SHIFT 14 // probabilities enter as p * (vs / E) * 2^14 < 2^15
 
 union Half8 {
@@ -270,17 +269,17 @@ __device__ __forceinline__ void load_q16(const Kv8Attn &a, bool wide, int64_t at
         }
     }
 }
-// Queries enter the products as halves.  They are scaled by one power of two for all rows that share it, so that the largest element
-// (mx) lies in [2^14, 2^15): a half then holds every bf16 element down to 2^-31 of the largest exactly, two halves hold 22 bits of an
-// fp32 one, and what smaller elements lose is 2^-39 of the largest - nothing in a score.
+// Queries are scaled by one power of two for all rows that share it, so that the largest element (mx) lies in [2^bits, 2^(bits + 1)).
 struct QScale {
-    float up, down; // to the halves, and back
+    float up, down; // there, and back
 };
-__device__ __forceinline__ QScale q_scale(float mx)
+__device__ __forceinline__ QScale q_scale(float mx, int bits)
 {
     const int e = min(127, max(-100, (int)(__float_as_uint(mx) >> 23) - 127)); // (kept where both factors are normal numbers)
-    return QScale{__uint_as_float((uint32_t)(127 + 14 - e) << 23), __uint_as_float((uint32_t)(127 - 14 + e) << 23)};
+    return QScale{__uint_as_float((uint32_t)(127 + bits - e) << 23), __uint_as_float((uint32_t)(127 - bits + e) << 23)};
 }
+// As halves (bits = 14): one holds every bf16 element down to 2^-31 of the largest exactly, two hold 22 bits of an fp32 one, and what
+// smaller elements lose is 2^-39 of the largest - nothing in a score.
 // The Q^T operands of a 16-row set: lane (qi, grp) takes dimensions 64 j + 16 grp + 8 s .. + 8 into step 2 j + s, the order a 16-byte
 // piece of the codes has them in.
 template <int HD, int TERMS>
@@ -299,19 +298,17 @@ __device__ __forceinline__ void query_operands(const float (&x)[HD / 4], float u
         if constexpr (TERMS == 2) q[1][s] = lo.v;
     }
 }
-// MT sets of 16 rows from product row m0 on (row i, head g of the group: m = i * grps + g); returns what a product has to be multiplied
-// by to be a score.
-template <int HD, int MT, int TERMS, typename MX>
-__device__ __forceinline__ float load_queries(const Kv8Attn &a, const Kv8Seq &sq, int n_rows, int kvh, int grps, int64_t m0, f16x8 (&q)[MT][TERMS][HD / 32],
-                                              MX all_max)
+// MT sets of 16 rows from product row m0 on (row i, head g of the group: m = i * grps + g), HD / 4 elements a lane: of dimensions
+// 64 j + 16 grp .. + 16 for each j.  Returns the largest magnitude.
+template <int HD, int MT, int TERMS>
+__device__ __forceinline__ float load_rows(const Kv8Attn &a, const Kv8Seq &sq, int n_rows, int kvh, int grps, int m0, float (&x)[MT][HD / 4])
 {
     const int qi = threadIdx.x & 15, grp = (threadIdx.x & 63) >> 4;
     const bool wide = kv8_wide(a.q, a.q_row, a.q_head, a.dtype);
-    float x[MT][HD / 4], mx = 0.f;
+    float mx = 0.f;
 #pragma unroll
     for (int mt = 0; mt < MT; mt++) {
-        const int64_t m = m0 + 16 * mt + qi;
-        const int i = (int)(m / grps), g = (int)(m % grps);
+        const int m = m0 + 16 * mt + qi, i = (unsigned)m / (unsigned)grps, g = m - i * grps;
 #pragma unroll
         for (int e = 0; e < HD / 4; e++) x[mt][e] = 0.f;
         if (i < n_rows) {
@@ -322,16 +319,151 @@ __device__ __forceinline__ float load_queries(const Kv8Attn &a, const Kv8Seq &sq
 #pragma unroll
         for (int e = 0; e < HD / 4; e++) mx = fmaxf(mx, fabsf(x[mt][e]));
     }
-    const QScale qs = q_scale(all_max(mx));
-#pragma unroll
-    for (int mt = 0; mt < MT; mt++) query_operands<HD, TERMS>(x[mt], qs.up, q[mt]);
-    return qs.down * a.scale;
+    return mx;
 }
 // over the wave
 __device__ __forceinline__ float wave_max(float v)
 {
     for (int o = 32; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
     return v;
+}
+
+// How the tiles of all (sequence, cache head, set of rows) units are dealt out.  Units stand in a row, a sequence's next to each other and as
+// long as what any row of the sequence sees; block b takes the stretch [b * chunk, (b + 1) * chunk), which may reach over several units
+// and cover parts of the first and the last: every block has the same work, whatever the lengths.  With too little work for that
+// (`cross` = false) units are rounded up to whole stretches instead, and no block has parts of two.
+// Tiles of a unit of sequence j and number of its units (each lane for a j of its own); {0, 0}: nothing to do.
+struct Kv8Units {
+    int T, n;
+};
+template <int SET>
+__device__ __forceinline__ Kv8Units kv8_units(const Kv8View &c, const Kv8Rows &rw, const Kv8Attn &a, int j)
+{
+    if (j >= rw.n) return Kv8Units{0, 0};
+    const int b = rw.seq_ids ? rw.seq_ids[j * rw.group] : j;
+    const int n_rows = rw.row_start ? rw.row_start[j + 1] - rw.row_start[j] : rw.rows; // (unused slots of the path count: they are written too)
+    if (b < 0 || b >= c.n_seq || n_rows < 1) return Kv8Units{0, 0};
+    const int T = kv8_tiles(a, kv8_length(rw.len[rw.path ? j * rw.group : b]), 0, n_rows - 1, kv8_capacity(c, b)).T;
+    return Kv8Units{max(T, 1), (n_rows * (a.n_heads / c.kv_heads) + SET - 1) / SET * c.kv_heads}; // (rows that see nothing are written: a tile at least)
+}
+__device__ __forceinline__ int64_t uniform64(int64_t v)
+{
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)v));
+}
+__device__ __forceinline__ int wave_total(int v)
+{
+    v += dpp_i<0xB1>(v), v += dpp_i<0x4E>(v), v += dpp_i<0x141>(v), v += dpp_i<0x140>(v);
+    return __builtin_amdgcn_readlane(v, 0) + __builtin_amdgcn_readlane(v, 16) + __builtin_amdgcn_readlane(v, 32) + __builtin_amdgcn_readlane(v, 48);
+}
+__device__ __forceinline__ int wave_most(int v)
+{
+    v = max(v, dpp_i<0xB1>(v)), v = max(v, dpp_i<0x4E>(v)), v = max(v, dpp_i<0x141>(v)), v = max(v, dpp_i<0x140>(v));
+    return max(max(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16)), max(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
+}
+__device__ __forceinline__ int wave_upto(int v) // sum of the lanes up to this one
+{
+    v += dpp_i<0x111>(v), v += dpp_i<0x112>(v), v += dpp_i<0x114>(v), v += dpp_i<0x118>(v);
+    const int a = __builtin_amdgcn_readlane(v, 15), b = __builtin_amdgcn_readlane(v, 31), c = __builtin_amdgcn_readlane(v, 47), row = (threadIdx.x & 63) >> 4;
+    return v + (row > 0 ? a : 0) + (row > 1 ? b : 0) + (row > 2 ? c : 0);
+}
+// The deal, and the first 64 sequences' share of it in the lanes.  2^31 tiles would be 8 TiB of codes.
+struct Kv8Deal {
+    int total, chunk; // tiles in the row, and of a stretch
+    bool cross;
+    Kv8Units mine;    // of sequence `lane`
+    int upto;         // where its units end
+    __device__ __forceinline__ int length(int T) const { return cross ? T : (int)(((unsigned)T + chunk - 1) / (unsigned)chunk) * chunk; }
+};
+// S: parts a unit may end up in; goal: blocks that are wanted.  Uniform over the grid.
+template <int SET>
+__device__ __forceinline__ Kv8Deal kv8_deal(const Kv8View &c, const Kv8Rows &rw, const Kv8Attn &a, int S, int goal)
+{
+    const int lane = threadIdx.x & 63;
+    Kv8Deal d;
+    d.mine = kv8_units<SET>(c, rw, a, lane);
+    int W = d.mine.T * d.mine.n, T_max = max(1, d.mine.T);
+    for (int j = lane + 64; j - lane < rw.n; j += 64) {
+        const Kv8Units u = kv8_units<SET>(c, rw, a, j);
+        W += u.T * u.n, T_max = max(T_max, u.T);
+    }
+    W = wave_total(W), T_max = wave_most(T_max);
+    d.cross = S > 1 && W > goal * K8_MIN_TILES;
+    // (a stretch that starts inside a unit makes one more part of it)
+    d.chunk = d.cross ? (int)max((unsigned)(W + goal - 1) / (unsigned)goal, (unsigned)(T_max + S - 2) / (unsigned)(S - 1))
+              : S > 1 ? max(K8_MIN_TILES, (int)((unsigned)(T_max + S - 1) / (unsigned)S)) : T_max;
+    const int len = d.length(d.mine.T) * d.mine.n;
+    d.upto = wave_upto(len);
+    d.total = W;
+    if (!d.cross) {
+        W = len;
+        for (int j = lane + 64; j - lane < rw.n; j += 64) {
+            const Kv8Units u = kv8_units<SET>(c, rw, a, j);
+            W += d.length(u.T) * u.n;
+        }
+        d.total = wave_total(W);
+    }
+    return d;
+}
+// The sequence that position `at` < total lies in, its unit's length, where its units start and end.
+struct Kv8Found {
+    int j, len, start, end;
+};
+template <int SET>
+__device__ __forceinline__ Kv8Found kv8_find(const Kv8View &c, const Kv8Rows &rw, const Kv8Attn &a, const Kv8Deal &d, int at)
+{
+    Kv8Units u = d.mine;
+    int upto = d.upto;
+    for (int j0 = 0, before = 0;; j0 += 64) {
+        const uint64_t behind = __ballot(upto > at);
+        if (behind || j0 + 64 >= rw.n) {
+            const int l = __builtin_amdgcn_readfirstlane(behind ? __ffsll((unsigned long long)behind) - 1 : 63);
+            const int len = d.length(__builtin_amdgcn_readlane(u.T, l)), end = __builtin_amdgcn_readlane(upto, l);
+            return Kv8Found{j0 + l, len, end - len * __builtin_amdgcn_readlane(u.n, l), end};
+        }
+        before = __builtin_amdgcn_readlane(upto, 63);
+        u = kv8_units<SET>(c, rw, a, j0 + 64 + (threadIdx.x & 63));
+        upto = before + wave_upto(d.length(u.T) * u.n);
+    }
+}
+
+// As integers of 22 bits (bits = 21) in three signed bytes, n = (d[2] * 256 + d[1]) * 256 + d[0]: the products with the codes are exact
+// integers, and the codes need no widening.  Lane (qi, grp) takes dimensions 64 j + 16 grp .. + 16 into step j, the order a 16-byte
+// piece of the codes has them in.
+typedef __attribute__((ext_vector_type(4))) int i32x4;
+template <int HD>
+__device__ __forceinline__ void query_digits(const float (&x)[HD / 4], float up, i32x4 (&q)[3][HD / 64])
+{
+#pragma unroll
+    for (int j = 0; j < HD / 64; j++)
+#pragma unroll
+        for (int w = 0; w < 4; w++) {
+            uint32_t n[4];
+#pragma unroll
+            for (int e = 0; e < 4; e++) // 1.5 * 2^23 + x rounds x to an integer and has it in its low bits; the bytes of n + 0x808080 are the digits + 128
+                n[e] = __float_as_uint(fmaf(x[16 * j + 4 * w + e], up, 12582912.f)) - (0x4b400000u - 0x00808080u);
+            const uint32_t a = __builtin_amdgcn_perm(n[1], n[0], 0x05010400u), b = __builtin_amdgcn_perm(n[3], n[2], 0x05010400u); // bytes 0, 0, 1, 1
+            const uint32_t c = __builtin_amdgcn_perm(n[1], n[0], 0x0c0c0602u), d = __builtin_amdgcn_perm(n[3], n[2], 0x0c0c0602u); // bytes 2, 2
+            q[0][j][w] = (int)(__builtin_amdgcn_perm(b, a, 0x05040100u) ^ 0x80808080u);
+            q[1][j][w] = (int)(__builtin_amdgcn_perm(b, a, 0x07060302u) ^ 0x80808080u);
+            q[2][j][w] = (int)(__builtin_amdgcn_perm(d, c, 0x05040100u) ^ 0x80808080u);
+        }
+}
+// maximum over a wave on the vector unit's own paths
+__device__ __forceinline__ float wave_max_dpp(float v)
+{
+    v = fmaxf(v, dpp_f<0xB1>(v));
+    v = fmaxf(v, dpp_f<0x4E>(v));
+    v = fmaxf(v, dpp_f<0x141>(v));
+    v = fmaxf(v, dpp_f<0x140>(v));
+    return rows4_max(v);
+}
+
+// Codes are read once per call: with the nontemporal hint.
+template <typename T>
+__device__ __forceinline__ T read_once(const int8_t *p)
+{
+    typedef __attribute__((ext_vector_type(sizeof(T) / 4))) uint32_t words;
+    return __builtin_bit_cast(T, __builtin_nontemporal_load((const words *)p));
 }
 
 // One wave's share of a tile's bytes, in flight while the tile before it is consumed.
@@ -342,49 +474,65 @@ struct K8Regs {
     };
     uint4 k[2][HD / 64];
     VRow v[8];
-    F4 ks[2], vs[2]; // tokens 4 grp .. + 4 and 16 + 4 grp .. + 4
+    float sc; // lanes 0..31: the K scale of the tile's token of that number, lanes 32..63: V scales
 };
 
 // Block: 4 waves over the tiles of one (sequence, cache head, set of MT * 16 rows, split), each with a running softmax of its own.
-//   S^T = K Q^T: two operands of 16 tokens each, read from the codes' rows in 16-byte pieces.  The result leaves lane (qi, grp)
+//   S^T = K Q^T in integers: two operands of 16 tokens each are the codes' rows as they lie, in 16-byte pieces; the queries are three
+//   signed bytes.  The result leaves lane (qi, grp)
 //   tokens 4 grp + r of both halves for row qi, which are the eight k-slots of the P^T operand of
 //   O^T = V^T P^T: V's rows are read as they lie (lane (m, grp): VB dimensions from VB m on of eight tokens) and transposed by
 //   the byte permutes that widen them.
 // E, a power of two above half the largest V scale so far, takes the scales' range out of the 16-bit probabilities.
 // Bound: memory; per code about 1.2 vector operations to widen it, beside one matrix instruction per 512 codes and 16 rows.
 template <int HD, int MT, int TERMS>
-__global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void kv8_attn_stream_kernel(Kv8View c, Kv8Rows rw, Kv8Attn a, int n_chunks, int S, int per_want, float *part)
+__global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void kv8_attn_stream_kernel(Kv8View c, Kv8Rows rw, Kv8Attn a, int S, int goal, float *part)
 {
-    constexpr int NS = HD / 32, VB = HD / 16, VW = HD / 64, ND = VB;
-    constexpr int DP = HD < 128 ? HD : 128; // dimensions merged at a time
-    __shared__ float sO[4][DP * 17];
+    constexpr int VB = HD / 16, VW = HD / 64, ND = VB, SET = 16 * MT;
+    __shared__ __attribute__((aligned(16))) float sO[4][16][HD + 4];
     __shared__ float sM[4][16], sL[4][16];
+    __shared__ __attribute__((aligned(16))) float sS[4][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int qi = lane & 15, grp = lane >> 4;
-    const int kvh = blockIdx.x % c.kv_heads, j = blockIdx.x / c.kv_heads % rw.n, chunk0 = blockIdx.x / c.kv_heads / rw.n, split = blockIdx.y;
-    const Kv8Seq sq = kv8_seq(c, rw, j);
     const int grps = a.n_heads / c.kv_heads;
-    if (sq.b < 0 && c.status && threadIdx.x == 0) atomicOr(c.status, 4);
-    const int n_rows = sq.b < 0 ? 0 : sq.n_rows;
-    const int64_t all = (int64_t)(rw.path ? rw.rows : n_rows) * grps; // (unused slots of the path receive zeros)
-    const int cap = sq.b < 0 ? 0 : c.cap[sq.b];
-    const int64_t base = (int64_t)kvh * c.tokens + (sq.b < 0 ? 0 : c.off[sq.b]);
-    const int8_t *K = c.k + base * HD, *V = c.v + base * HD;
-    const float *KS = c.ks + base, *VS = c.vs + base;
-    for (int64_t m0 = (int64_t)chunk0 * MT * 16; m0 < all; m0 += (int64_t)n_chunks * MT * 16) {
-        const int i_first = (int)(m0 / grps), i_last = (int)min((int64_t)n_rows - 1, (m0 + MT * 16 - 1) / grps);
+    if (blockIdx.x == 0 && c.status) // sequence ids out of range have no units
+        for (int j = threadIdx.x; j < rw.n; j += 256)
+            if (rw.seq_ids && (rw.seq_ids[j * rw.group] < 0 || rw.seq_ids[j * rw.group] >= c.n_seq)) atomicOr(c.status, 4);
+    const Kv8Deal deal = kv8_deal<SET>(c, rw, a, S, goal);
+    Kv8Found f = {0, 1, 0, 0};
+    for (int blk = blockIdx.x; blk * deal.chunk < deal.total; blk += gridDim.x)
+    for (int at = blk * deal.chunk, end = min(at + deal.chunk, deal.total); at < end;) {
+        // the unit that position `at` lies in, and this block's part of it
+        if (at >= f.end || at < f.start) f = kv8_find<SET>(c, rw, a, deal, at);
+        const int j = f.j, unit = (unsigned)(at - f.start) / (unsigned)f.len;
+        const int u0 = f.start + unit * f.len; // the unit's first position
+        const int t_begin = at - u0, first_blk = (unsigned)u0 / (unsigned)deal.chunk, split = blk - first_blk;
+        const bool only = u0 + f.len <= (first_blk + 1) * deal.chunk; // the whole unit is this block's
+        const int set = (unsigned)unit / (unsigned)c.kv_heads, kvh = unit - set * c.kv_heads, m0 = set * SET;
+        const int n_here = min(end, u0 + f.len) - at;
+        at += n_here;
+        const Kv8Seq sq = kv8_seq(c, rw, j);
+        const int n_rows = sq.n_rows, all = (rw.path ? rw.rows : n_rows) * grps; // (unused slots of the path receive zeros)
+        const int cap = kv8_capacity(c, sq.b);
+        const int64_t base = uniform64((int64_t)kvh * c.tokens + c.off[sq.b]);
+        const int8_t *K = c.k + base * HD, *V = c.v + base * HD;
+        const float *KS = c.ks + base, *VS = c.vs + base;
+        // (tiles are those of the whole sequence, so that a unit's parts are known without its rows; what the set's rows see bounds them)
+        const int i_first = (unsigned)m0 / (unsigned)grps, i_last = min(n_rows - 1, (int)((unsigned)(m0 + SET - 1) / (unsigned)grps));
         Kv8Tiles tl = {};
-        if (i_first < n_rows) tl = kv8_tiles(a, sq.len, i_first, i_last, cap);
-        const int per = kv8_per_split(tl.T, S, per_want), t_begin = split * per, t_end = min(tl.T, t_begin + per);
-        if (split > 0 && t_begin >= tl.T) continue;
-        f16x8 q[MT][TERMS][NS];
-        const float qf = load_queries<HD, MT, TERMS>(a, sq, n_rows, kvh, grps, m0, q, wave_max); // (the same for every wave: they hold the same rows)
+        if (i_first < n_rows) {
+            tl = kv8_tiles(a, sq.len, 0, (rw.row_start ? n_rows : rw.rows) - 1, cap);
+            const Kv8Seen first = kv8_seen(a, sq.len, i_first, cap), last = kv8_seen(a, sq.len, i_last, cap);
+            tl.hi_min = first.hi, tl.lo_max = last.lo;
+            tl.hi_max = last.hi;
+        }
+        const int t_end = min(min(tl.T, tl.n_sink + (tl.hi_max + K8_TILE - 1) / K8_TILE - tl.w0), t_begin + n_here);
         float m_run[MT], l_run[MT];
         Kv8Seen seen[MT]; // of the lane's row in each set
         f32x4 o[MT][ND];
 #pragma unroll
         for (int mt = 0; mt < MT; mt++) {
-            const int i = (int)((m0 + 16 * mt + qi) / grps);
+            const int i = (unsigned)(m0 + 16 * mt + qi) / (unsigned)grps;
             seen[mt] = kv8_seen(a, sq.len, i, cap);
             if (i >= n_rows) seen[mt] = Kv8Seen{0, 0, 0};
             m_run[mt] = -INFINITY, l_run[mt] = 0.f;
@@ -404,74 +552,81 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void kv8_attn_stream_kernel(K
 #pragma unroll
                 for (int h = 0; h < 2; h++)
 #pragma unroll
-                    for (int p = 0; p < HD / 64; p++) r.k[h][p] = *(const uint4 *)(kt + k_lane + (16 * h * HD + 64 * p));
-#pragma unroll
-                for (int h = 0; h < 2; h++) r.ks[h] = *(const F4 *)(KS + t0 + 16 * h + 4 * grp), r.vs[h] = *(const F4 *)(VS + t0 + 16 * h + 4 * grp);
+                    for (int p = 0; p < HD / 64; p++) r.k[h][p] = read_once<uint4>(kt + k_lane + (16 * h * HD + 64 * p));
             } else { // tokens behind the last one any row sees repeat that one
 #pragma unroll
                 for (int h = 0; h < 2; h++)
 #pragma unroll
                     for (int p = 0; p < HD / 64; p++) r.k[h][p] = *(const uint4 *)(K + (int64_t)min(t0 + 16 * h + qi, last_tok) * HD + 64 * p + 16 * grp);
-#pragma unroll
-                for (int e = 0; e < 8; e++) {
-                    const int tok = min(t0 + 16 * (e / 4) + 4 * grp + e % 4, last_tok);
-                    r.ks[e / 4].v[e % 4] = KS[tok], r.vs[e / 4].v[e % 4] = VS[tok];
-                }
             }
+            const int tok = t0 + (lane & 31);
+            r.sc = (lane < 32 ? KS : VS)[min(tok, last_tok)];
         };
         auto load_v = [&](int t) {
             const int t0 = tl.token0(t);
             if (t0 + K8_TILE <= tl.hi_max) {
                 const int8_t *vt = V + (int64_t)t0 * HD;
 #pragma unroll
-                for (int e = 0; e < 8; e++) r.v[e] = *(const typename K8Regs<HD>::VRow *)(vt + v_lane + (e < 4 ? e : 12 + e) * HD);
+                for (int e = 0; e < 8; e++) r.v[e] = read_once<typename K8Regs<HD>::VRow>(vt + v_lane + (e < 4 ? e : 12 + e) * HD);
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; e++)
                     r.v[e] = *(const typename K8Regs<HD>::VRow *)(V + (int64_t)min(t0 + 16 * (e / 4) + 4 * grp + e % 4, last_tok) * HD + VB * qi);
             }
         };
-        auto consume = [&](int t, int t_next, auto masked) { // t_next < 0: none
+        const Kv8Order od = kv8_order(tl, t_begin, t_end);
+        if (wave < od.n) { // the first tile is on its way while the queries are read
+            load_k(od.tile(wave));
+            load_v(od.tile(wave));
+        }
+        i32x4 q[MT][3][HD / 64];
+        float qf; // what a product has to be multiplied by to be a score
+        {
+            float x[MT][HD / 4];
+            const QScale qs = q_scale(wave_max_dpp(load_rows<HD, MT, TERMS>(a, sq, n_rows, kvh, grps, m0, x)), 21); // (the same in every wave: they hold the same rows)
+            qf = qs.down * a.scale;
+#pragma unroll
+            for (int mt = 0; mt < MT; mt++) query_digits<HD>(x[mt], qs.up, q[mt]);
+        }
+        // (t_next is asked for whether it is wanted or not: with loads that may be left out, the wait for K would have to be one for V too)
+        auto consume = [&](int t, int t_next, auto masked) {
             constexpr bool MASKED = decltype(masked)::value;
             const int rel = tl.token0(t) + 4 * grp; // tokens are counted from the lane's first one
-            f32x4 s[MT][2];
-#pragma unroll
-            for (int mt = 0; mt < MT; mt++) s[mt][0] = s[mt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int h = 0; h < 2; h++)
-#pragma unroll
-                for (int p = 0; p < HD / 64; p++) {
-                    const f16x8 k0 = codes_to_half(r.k[h][p].x, r.k[h][p].y), k1 = codes_to_half(r.k[h][p].z, r.k[h][p].w);
-#pragma unroll
-                    for (int mt = 0; mt < MT; mt++)
-#pragma unroll
-                        for (int w = 0; w < TERMS; w++) {
-                            s[mt][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, q[mt][w][2 * p], s[mt][h], 0, 0, 0);
-                            s[mt][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, q[mt][w][2 * p + 1], s[mt][h], 0, 0, 0);
-                        }
-                }
-            float ks[8], vs[8], big = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; e++) {
-                ks[e] = r.ks[e / 4].v[e % 4] * qf;
-                vs[e] = r.vs[e / 4].v[e % 4];
-                if (MASKED) { // scales of tokens that no row sees are not looked at
-                    const int tok = 16 * (e / 4) + e % 4;
-                    if (!(tok < tl.hi_max - rel && (tok >= tl.lo_min - rel || tok < a.sinks - rel))) vs[e] = 0.f;
-                }
-                big = fmaxf(big, vs[e]);
+            float sc = r.sc;
+            if (MASKED) { // V scales of tokens that no row sees are not looked at
+                const int tok = tl.token0(t) + (lane & 31);
+                if (lane >= 32 && !(tok < tl.hi_max && (tok >= tl.lo_min || tok < a.sinks))) sc = 0.f;
             }
-            __builtin_amdgcn_sched_barrier(0);
-            if (t_next >= 0) load_k(t_next);
-            __builtin_amdgcn_sched_barrier(0);
-            // the tile's V scales over E
-            big = __uint_as_float(min(__float_as_uint(rows4_max(big)), 0x7e000000u) & 0x7f800000u);
+            // the tile's V scales over E, and the scales to the lanes that need them (the LDS takes a wave's accesses in order)
+            const float big = __uint_as_float(min(__float_as_uint(wave_max_dpp(lane < 32 ? 0.f : sc)), 0x7e000000u) & 0x7f800000u);
             const float E_new = fmaxf(E, big);
             const float inv = __uint_as_float(0x7f000000u + (K8_P_SHIFT << 23) - __float_as_uint(E_new));
             const float shrink = E * __uint_as_float(0x7f000000u - __float_as_uint(E_new));
             E = E_new;
+            sS[wave][lane] = sc * (lane < 32 ? qf : inv);
+            asm volatile("" ::: "memory");
+            f32x4 s[MT][2];
 #pragma unroll
-            for (int e = 0; e < 8; e++) vs[e] *= inv;
+            for (int h = 0; h < 2; h++)
+#pragma unroll
+                for (int mt = 0; mt < MT; mt++) {
+                    i32x4 d[3];
+#pragma unroll
+                    for (int k = 0; k < 3; k++) {
+                        d[k] = i32x4{0, 0, 0, 0};
+#pragma unroll
+                        for (int p = 0; p < HD / 64; p++)
+                            d[k] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, r.k[h][p]), q[mt][k][p], d[k], 0, 0, 0);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; e++) s[mt][h][e] = fmaf((float)((d[2][e] << 8) + d[1][e]), 256.f, (float)d[0][e]);
+                }
+            const f32x4 ka = *(const f32x4 *)&sS[wave][4 * grp], kb = *(const f32x4 *)&sS[wave][16 + 4 * grp];
+            const f32x4 va = *(const f32x4 *)&sS[wave][32 + 4 * grp], vb = *(const f32x4 *)&sS[wave][48 + 4 * grp];
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+            load_k(t_next);
+            __builtin_amdgcn_sched_barrier(0);
             Half8 ph[MT][TERMS];
 #pragma unroll
             for (int mt = 0; mt < MT; mt++) {
@@ -480,7 +635,7 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void kv8_attn_stream_kernel(K
                 const int hi = seen[mt].hi - rel, lo = seen[mt].lo - rel, sk = a.sinks - rel;
 #pragma unroll
                 for (int e = 0; e < 8; e++) {
-                    x[e] = s[mt][e / 4][e % 4] * ks[e];
+                    x[e] = s[mt][e / 4][e % 4] * (e < 4 ? ka[e] : kb[e - 4]);
                     if (MASKED) {
                         const int tok = 16 * (e / 4) + e % 4;
                         vis[e] = tok < hi && (tok >= lo || tok < sk);
@@ -500,7 +655,7 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void kv8_attn_stream_kernel(K
                     for (int f = 0; f < 2; f++) {
                         p[f] = __builtin_amdgcn_exp2f(x[e + f] - ref);
                         sum += p[f];
-                        p[f] *= vs[e + f];
+                        p[f] *= e < 4 ? va[e + f] : vb[e - 4 + f];
                         if (MASKED) p[f] = vis[e + f] ? p[f] : 0.f;
                     }
                     ph[mt][0].h[e / 2] = half2_of(p[0], p[1]);
@@ -536,60 +691,62 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void kv8_attn_stream_kernel(K
                             o[mt][4 * w + b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[b].v, ph[mt][u].v, o[mt][4 * w + b], 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            if (t_next >= 0) load_v(t_next);
+            load_v(t_next);
             __builtin_amdgcn_sched_barrier(0);
         };
-        const Kv8Order od = kv8_order(tl, t_begin, t_end);
         if (wave < od.n) {
             int u = wave;
-            load_k(od.tile(u));
-            load_v(od.tile(u));
-            for (; u < od.n_edge; u += 4) consume(od.tile(u), u + 4 < od.n ? od.tile(u + 4) : -1, std::true_type{});
-            for (; u < od.n; u += 4) consume(od.tile(u), u + 4 < od.n ? od.tile(u + 4) : -1, std::false_type{});
+            for (; u < od.n_edge; u += 4) consume(od.tile(u), od.tile(min(u + 4, od.n - 1)), std::true_type{});
+            for (; u < od.n; u += 4) consume(od.tile(u), od.tile(min(u + 4, od.n - 1)), std::false_type{});
         }
-        // the waves' parts meet: O in true units (E and the shifts undone), weighted by their maxima
-        const float unit = E * 0.03125f; // 2^(9 - 14)
+        // the waves' parts meet: O in true units (E and the shifts undone), weighted by their maxima.  Thread (row, c) of the sum holds
+        // VB adjacent dimensions of a row.
+        const float back = E * 0.03125f; // 2^(9 - 14)
+        const int row = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * VB;
 #pragma unroll
         for (int mt = 0; mt < MT; mt++) {
             const float l = rows4_sum(l_run[mt]);
+            __syncthreads(); // what was there has been read
+            if (grp == 0) sM[wave][qi] = m_run[mt], sL[wave][qi] = l;
 #pragma unroll
-            for (int d0 = 0; d0 < HD; d0 += DP) { // (a pass holds the accumulators of VB / (HD / DP) bytes of each lane's dimensions)
-                __syncthreads();
-                if (grp == 0 && d0 == 0) sM[wave][qi] = m_run[mt], sL[wave][qi] = l;
-                constexpr int NB = VB / (HD / DP);
+            for (int r = 0; r < 4; r++)
 #pragma unroll
-                for (int b = 0; b < NB; b++)
+                for (int b = 0; b < VB; b += 4)
+                    *(f32x4 *)&sO[wave][qi][VB * (4 * grp + r) + b] =
+                        f32x4{o[mt][b][r], o[mt][b + 1][r], o[mt][b + 2][r], o[mt][b + 3][r]} * back;
+            __syncthreads();
+            const int m = m0 + 16 * mt + row;
+            if (m >= all) continue;
+            const float M = fmaxf(fmaxf(sM[0][row], sM[1][row]), fmaxf(sM[2][row], sM[3][row])), ref = M == -INFINITY ? 0.f : M;
+            float v[VB], L = 0.f;
 #pragma unroll
-                    for (int r = 0; r < 4; r++) sO[wave][(NB * (4 * grp + r) + b) * 17 + qi] = o[mt][d0 / DP * NB + b][r] * unit;
-                __syncthreads();
-                for (int u = threadIdx.x; u < DP * 16; u += 256) {
-                    const int dd = u % DP, row = u / DP;
-                    const int d = VB * (dd / NB) + d0 / DP * NB + dd % NB;
-                    const int64_t m = m0 + 16 * mt + row;
-                    if (m >= all) continue;
-                    const float M = fmaxf(fmaxf(sM[0][row], sM[1][row]), fmaxf(sM[2][row], sM[3][row])), ref = M == -INFINITY ? 0.f : M;
-                    float O = 0.f, L = 0.f;
+            for (int d = 0; d < VB; d++) v[d] = 0.f;
 #pragma unroll
-                    for (int w = 0; w < 4; w++) {
-                        const float f = __builtin_amdgcn_exp2f(sM[w][row] - ref);
-                        O += sO[w][dd * 17 + row] * f;
-                        L += sL[w][row] * f;
-                    }
-                    const int i = (int)(m / grps), h = kvh * grps + (int)(m % grps), r = sq.row0 + i;
-                    if (i >= n_rows) kv8_store_out(a, r, h, HD, d, 0.f); // an unused slot of the path
-                    else if (tl.T <= per) { // one split: this is the result
-                        // (nothing seen: L is 0.  A sum that is not a number stays one.)
-                        kv8_store_out(a, r, h, HD, d, L == 0.f ? 0.f : O / L);
-                        if (a.lse && d == 0) a.lse[(int64_t)r * a.n_heads + h] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
-                    } else {
-                        float *p = part + (((int64_t)r * a.n_heads + h) * S + split) * (HD + 4);
-                        p[4 + d] = O;
-                        if (d == 0) p[0] = M, p[1] = L;
-                    }
+            for (int w = 0; w < 4; w++) {
+                const float g = __builtin_amdgcn_exp2f(sM[w][row] - ref);
+                L = fmaf(sL[w][row], g, L);
+#pragma unroll
+                for (int d = 0; d < VB; d += 4) {
+                    const f32x4 x = *(const f32x4 *)&sO[w][row][d0 + d];
+#pragma unroll
+                    for (int e = 0; e < 4; e++) v[d + e] = fmaf(x[e], g, v[d + e]);
                 }
             }
+            const int i = (unsigned)m / (unsigned)grps, h = kvh * grps + (m - i * grps), r = sq.row0 + i;
+            if (only || i >= n_rows) { // this is the result (of an unused slot of the path: zeros)
+                // (nothing seen: L is 0.  A sum that is not a number stays one.)
+                const float g = L == 0.f || i >= n_rows ? 0.f : 1.0f / L;
+#pragma unroll
+                for (int d = 0; d < VB; d++) v[d] = i >= n_rows ? 0.f : v[d] * g;
+                kv8_store_run<VB>(a, kv8_wide(a.out, a.o_row, a.o_head, a.dtype), r, h, HD, d0, v);
+                if (a.lse && d0 == 0) a.lse[(int64_t)r * a.n_heads + h] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
+            } else {
+                float *p = part + (((int64_t)r * a.n_heads + h) * S + split) * (HD + 4);
+#pragma unroll
+                for (int d = 0; d < VB; d += 4) *(float4 *)(p + 4 + d0 + d) = make_float4(v[d], v[d + 1], v[d + 2], v[d + 3]);
+                if (d0 == 0) p[0] = M, p[1] = L;
+            }
         }
-        __syncthreads();
     }
 }
 
@@ -623,19 +780,14 @@ __global__ __launch_bounds__(256, 3) void kv8_attn_tile_kernel(Kv8View c, Kv8Row
     {
         int b = blockIdx.x / c.kv_heads;
         if (!rw.row_start) {
-            const int sets = (int)(((int64_t)rw.rows * grps + ROWS - 1) / ROWS);
+            const int sets = (rw.rows * grps + ROWS - 1) / ROWS;
             j = b % rw.n, chunk = sets - 1 - b / rw.n;
         } else { // sets of every sequence, counted by the lanes
             int found = -1, left = b;
             for (int j0 = 0; j0 < rw.n && found < 0; j0 += 64) {
                 const int jj = j0 + lane;
                 const int n = jj < rw.n ? rw.row_start[jj + 1] - rw.row_start[jj] : 0;
-                const int sets = n > 0 ? (int)(((int64_t)n * grps + ROWS - 1) / ROWS) : 0;
-                int upto = sets; // of the lanes up to this one
-                for (int o = 1; o < 64; o <<= 1) {
-                    const int v = __shfl_up(upto, o, 64);
-                    if (lane >= o) upto += v;
-                }
+                const int upto = wave_upto(n > 0 ? (n * grps + ROWS - 1) / ROWS : 0);
                 const uint64_t behind = __ballot(upto > left);
                 if (behind) {
                     const int l = __ffsll((unsigned long long)behind) - 1;
@@ -650,19 +802,19 @@ __global__ __launch_bounds__(256, 3) void kv8_attn_tile_kernel(Kv8View c, Kv8Row
     const Kv8Seq sq = kv8_seq(c, rw, j);
     if (sq.b < 0 && c.status && threadIdx.x == 0) atomicOr(c.status, 4);
     const int n_rows = sq.b < 0 ? 0 : sq.n_rows;
-    const int64_t all = (int64_t)(rw.path ? rw.rows : n_rows) * grps, m_blk = (int64_t)chunk * ROWS, m0 = m_blk + wave * (MT * 16);
+    const int all = (rw.path ? rw.rows : n_rows) * grps, m_blk = chunk * ROWS, m0 = m_blk + wave * (MT * 16);
     if (m_blk >= all) return;
-    const int cap = sq.b < 0 ? 0 : c.cap[sq.b];
-    const int64_t base = (int64_t)kvh * c.tokens + (sq.b < 0 ? 0 : c.off[sq.b]);
+    const int cap = sq.b < 0 ? 0 : kv8_capacity(c, sq.b);
+    const int64_t base = uniform64((int64_t)kvh * c.tokens + (sq.b < 0 ? 0 : c.off[sq.b]));
     const int8_t *K = c.k + base * HD, *V = c.v + base * HD;
     const float *KS = c.ks + base, *VS = c.vs + base;
-    const int i_first = (int)(m_blk / grps), i_last = (int)min((int64_t)n_rows - 1, (m_blk + ROWS - 1) / grps);
+    const int i_first = (unsigned)m_blk / (unsigned)grps, i_last = min(n_rows - 1, (int)((unsigned)(m_blk + ROWS - 1) / (unsigned)grps));
     Kv8Tiles tl = {};
     if (i_first < n_rows) tl = kv8_tiles(a, sq.len, i_first, i_last, cap);
     const int per = kv8_per_split(tl.T, S, per_want), t_begin = split * per, t_end = min(tl.T, t_begin + per);
     if (split > 0 && t_begin >= tl.T) return;
     // what the wave's rows see
-    const int w_first = (int)(m0 / grps), w_last = (int)min((int64_t)n_rows - 1, (m0 + MT * 16 - 1) / grps);
+    const int w_first = (unsigned)m0 / (unsigned)grps, w_last = min(n_rows - 1, (int)((unsigned)(m0 + MT * 16 - 1) / (unsigned)grps));
     Kv8Tiles wt = {};
     if (w_first < n_rows) wt = kv8_tiles(a, sq.len, w_first, w_last, cap);
     auto block_max = [&](float v) {
@@ -673,13 +825,20 @@ __global__ __launch_bounds__(256, 3) void kv8_attn_tile_kernel(Kv8View c, Kv8Row
         return fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
     };
     f16x8 q[MT][TERMS][NS];
-    const float qf = load_queries<HD, MT, TERMS>(a, sq, n_rows, kvh, grps, m0, q, block_max);
+    float qf; // what a product has to be multiplied by to be a score
+    {
+        float x[MT][HD / 4];
+        const QScale qs = q_scale(block_max(load_rows<HD, MT, TERMS>(a, sq, n_rows, kvh, grps, m0, x)), 14);
+        qf = qs.down * a.scale;
+#pragma unroll
+        for (int mt = 0; mt < MT; mt++) query_operands<HD, TERMS>(x[mt], qs.up, q[mt]);
+    }
     float m_run[MT], l_run[MT];
     Kv8Seen seen[MT];
     f32x4 o[MT][ND];
 #pragma unroll
     for (int mt = 0; mt < MT; mt++) {
-        const int i = (int)((m0 + 16 * mt + qi) / grps);
+        const int i = (unsigned)(m0 + 16 * mt + qi) / (unsigned)grps;
         seen[mt] = kv8_seen(a, sq.len, i, cap);
         if (i >= n_rows) seen[mt] = Kv8Seen{0, 0, 0};
         m_run[mt] = -INFINITY, l_run[mt] = 0.f;
@@ -858,9 +1017,9 @@ __global__ __launch_bounds__(256, 3) void kv8_attn_tile_kernel(Kv8View c, Kv8Row
 #pragma unroll
     for (int mt = 0; mt < MT; mt++) {
         const float l = rows4_sum(l_run[mt]);
-        const int64_t m = m0 + 16 * mt + qi;
+        const int m = m0 + 16 * mt + qi;
         if (m >= all) continue;
-        const int i = (int)(m / grps), h = kvh * grps + (int)(m % grps), r = sq.row0 + i;
+        const int i = (unsigned)m / (unsigned)grps, h = kvh * grps + (m - i * grps), r = sq.row0 + i;
         if (i >= n_rows) { // an unused slot of the path
 #pragma unroll
             for (int k = 0; k < 4; k++) kv8_store_run<VB>(a, wide, r, h, HD, VB * (4 * grp + k), {});
@@ -888,65 +1047,107 @@ __global__ __launch_bounds__(256, 3) void kv8_attn_tile_kernel(Kv8View c, Kv8Row
     }
 }
 
-// Joins the splits of one (row, head).
+// ---------------------------------------------------------------- parts of a context meet
+// HD / 4 threads per product row; parts lie one after the other, { maximum, sum, -, -, HD outputs } each.
 template <int HD>
-__global__ __launch_bounds__(HD) void kv8_attn_join_kernel(Kv8View c, Kv8Rows rw, Kv8Attn a, int set_rows, int S, int per_want, const float *__restrict__ part)
+__device__ __forceinline__ void kv8_join_row(const Kv8Attn &a, int r, int h, int used, int S, const float *part)
 {
-    const int r = blockIdx.x, h = blockIdx.y, d = threadIdx.x;
+    const int dg = threadIdx.x % (HD / 4);
+    const float *p = part + ((int64_t)r * a.n_heads + h) * S * (HD + 4);
+    float M = -INFINITY, L = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+    for (int s = 0; s < used; s++) M = fmaxf(M, p[s * (HD + 4)]);
+    const float ref = M == -INFINITY ? 0.f : M;
+#pragma unroll 8
+    for (int s = 0; s < used; s++) {
+        const float2 ml = *(const float2 *)(p + s * (HD + 4));
+        const float4 w = *(const float4 *)(p + s * (HD + 4) + 4 + 4 * dg);
+        const float f = __builtin_amdgcn_exp2f(ml.x - ref);
+        L = fmaf(ml.y, f, L);
+        o.x = fmaf(w.x, f, o.x), o.y = fmaf(w.y, f, o.y), o.z = fmaf(w.z, f, o.z), o.w = fmaf(w.w, f, o.w);
+    }
+    const float inv = L == 0.f ? 0.f : 1.0f / L;
+    const float v[4] = {o.x * inv, o.y * inv, o.z * inv, o.w * inv};
+    kv8_store_run<4>(a, kv8_wide(a.out, a.o_row, a.o_head, a.dtype), r, h, HD, 4 * dg, v);
+    if (a.lse && dg == 0) a.lse[(int64_t)r * a.n_heads + h] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
+}
+
+// Of kv8_attn_stream_kernel<HD, SET / 16, ..>: a block takes 1024 / HD product rows of one (sequence, cache head) at a time.
+template <int HD, int SET>
+__global__ __launch_bounds__(256) void kv8_attn_join_kernel(Kv8View c, Kv8Rows rw, Kv8Attn a, int n_groups, int S, int goal, const float *__restrict__ part)
+{
+    constexpr int NG = 1024 / HD;
+    const int kvh = blockIdx.x % c.kv_heads, j = blockIdx.x / c.kv_heads % rw.n, g0 = blockIdx.x / c.kv_heads / rw.n;
+    const Kv8Deal deal = kv8_deal<SET>(c, rw, a, S, goal);
+    int u0 = 0, T = 0; // where the sequence's units start, and their tiles
+    for (int k = threadIdx.x & 63, first = 1; k - (int)(threadIdx.x & 63) <= j; k += 64, first = 0) {
+        const Kv8Units u = first ? deal.mine : kv8_units<SET>(c, rw, a, k);
+        u0 += k < j ? deal.length(u.T) * u.n : 0;
+        T += k == j ? u.T : 0;
+    }
+    u0 = wave_total(u0), T = wave_total(T);
+    if (T == 0) return;
+    const Kv8Seq sq = kv8_seq(c, rw, j);
+    const int grps = a.n_heads / c.kv_heads, len = deal.length(T);
+    for (int m = g0 * NG + threadIdx.x / (HD / 4); m < sq.n_rows * grps; m += n_groups * NG) {
+        const int at = u0 + (m / SET * c.kv_heads + kvh) * len;
+        const int used = (unsigned)(at + len - 1) / (unsigned)deal.chunk - (unsigned)at / (unsigned)deal.chunk + 1, i = (unsigned)m / (unsigned)grps;
+        if (used > 1) kv8_join_row<HD>(a, sq.row0 + i, kvh * grps + (m - i * grps), used, S, part); // (else the result is there)
+    }
+}
+
+// Of kv8_attn_tile_kernel<HD, 2, ..>: 1024 / HD (row, head) pairs per block.
+template <int HD>
+__global__ __launch_bounds__(256) void kv8_attn_join_tiles_kernel(Kv8View c, Kv8Rows rw, Kv8Attn a, int S, int per_want, const float *__restrict__ part)
+{
+    constexpr int NG = 1024 / HD, SET = 128;
+    const int r = blockIdx.x, h = blockIdx.y * NG + threadIdx.x / (HD / 4);
     const int j = kv8_owner(rw, r);
     if (j < 0 || j >= rw.n) return;
     const Kv8Seq sq = kv8_seq(c, rw, j);
     const int i = r - sq.row0, grps = a.n_heads / c.kv_heads;
-    if (sq.b < 0 || i >= sq.n_rows) return;
-    const int64_t m0 = ((int64_t)i * grps + h % grps) / set_rows * set_rows; // the set of rows that the row went with
-    const int i_last = (int)min((int64_t)sq.n_rows - 1, (m0 + set_rows - 1) / grps);
-    const int T = kv8_tiles(a, sq.len, (int)(m0 / grps), i_last, c.cap[sq.b]).T, per = kv8_per_split(T, S, per_want), used = (T + per - 1) / per;
-    if (used <= 1) return; // the block has written the result
-    const float *p = part + ((int64_t)r * a.n_heads + h) * S * (HD + 4);
-    float M = -INFINITY;
-    for (int s = 0; s < used; s++) M = fmaxf(M, p[s * (HD + 4)]);
-    const float ref = M == -INFINITY ? 0.f : M;
-    float O = 0.f, L = 0.f;
-    for (int s = 0; s < used; s++) {
-        const float f = __builtin_amdgcn_exp2f(p[s * (HD + 4)] - ref);
-        O += p[s * (HD + 4) + 4 + d] * f;
-        L += p[s * (HD + 4) + 1] * f;
-    }
-    kv8_store_out(a, r, h, HD, d, L == 0.f ? 0.f : O / L);
-    if (a.lse && d == 0) a.lse[(int64_t)r * a.n_heads + h] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
+    if (sq.b < 0 || i >= sq.n_rows || h >= a.n_heads) return;
+    const int set0 = (i * grps + h % grps) / SET * SET; // the set of rows that the row went with
+    const int T = kv8_tiles(a, sq.len, set0 / grps, min(sq.n_rows - 1, (set0 + SET - 1) / grps), kv8_capacity(c, sq.b)).T;
+    const int per = kv8_per_split(T, S, per_want), used = (T + per - 1) / per;
+    if (used > 1) kv8_join_row<HD>(a, r, h, used, S, part);
 }
 
 // ---------------------------------------------------------------- which kernel, how many blocks
-#define K8_MIN_TILES 16
-#define K8_MAX_SPLITS 64
 enum Kv8Kernel { KV8_PLAIN, KV8_STREAM, KV8_TILES };
 struct Kv8Plan {
-    int kernel, mt, set_rows, splits, per; // 16-row sets of a wave; product rows of a block; splits of a context and tiles of one
-    int64_t blocks;                   // per cache head and split
+    int kernel, mt, splits; // 16-row sets of a wave; parts that a context may be in
+    int goal, per;          // KV8_STREAM: blocks wanted; KV8_TILES: tiles of a split
+    int64_t blocks, max_m;  // launched (KV8_TILES: per split); product rows of a sequence, as far as is known
 };
 static Kv8Plan kv8_plan(const Kv8View &c, const Kv8Rows &rw, const Kv8Attn &a, int64_t ws_bytes)
 {
-    Kv8Plan p = {KV8_PLAIN, 0, 0, 1, 0, 0};
+    Kv8Plan p = {KV8_PLAIN, 0, 1, 0, 0, 0, 0};
     if ((g_force_generic & 2) || (c.hd != 64 && c.hd != 128)) return p;
     const int64_t max_rows = a.max_rows > 0 ? std::min(a.max_rows, a.total_rows) : a.total_rows, grps = a.n_heads / c.kv_heads;
     const int64_t R = max_rows * grps; // product rows of a sequence
-    int64_t goal; // blocks wanted on the chip
-    if (R <= 32) {
-        p.kernel = KV8_STREAM, p.mt = R <= 16 ? 1 : 2, p.set_rows = 16 * p.mt;
-        p.blocks = rw.n * ((R + p.set_rows - 1) / p.set_rows);
-        goal = 2048;
-    } else {
-        p.kernel = KV8_TILES, p.mt = 2, p.set_rows = 64 * p.mt;
-        p.blocks = rw.row_start ? a.total_rows * grps / p.set_rows + rw.n : rw.n * ((R + p.set_rows - 1) / p.set_rows);
-        goal = 512;
-    }
     const int64_t tokens = a.window ? std::min<int64_t>((int64_t)a.window + a.sinks + max_rows, (int64_t)a.max_len + max_rows) : (int64_t)a.max_len + max_rows;
-    const int64_t tiles = (tokens + K8_TILE - 1) / K8_TILE, blocks = p.blocks * c.kv_heads;
-    // a split takes K8_MIN_TILES tiles at least and the context K8_MAX_SPLITS splits at most
-    p.per = (int)std::max(std::max<int64_t>((tiles * blocks + goal - 1) / goal, (tiles + K8_MAX_SPLITS - 1) / K8_MAX_SPLITS), (int64_t)K8_MIN_TILES);
-    p.splits = (int)std::max<int64_t>(1, (tiles + p.per - 1) / p.per);
-    const int64_t one = (int64_t)a.total_rows * a.n_heads * (c.hd + 4) * sizeof(float);
-    if (ws_bytes >= 0 && p.splits > 1) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(p.splits, ws_bytes / one));
+    const int64_t tiles = (tokens + K8_TILE - 1) / K8_TILE;
+    const int64_t one = (int64_t)a.total_rows * a.n_heads * (c.hd + 4) * sizeof(float); // workspace of a split
+    if (R <= 32) {
+        p.kernel = KV8_STREAM, p.mt = R <= 16 ? 1 : 2, p.max_m = R;
+        const int64_t units = (int64_t)rw.n * c.kv_heads;
+        // the blocks that 256 compute units hold at once; a unit in about as many parts as there are blocks for it (twice that, and one
+        // more at either end, where lengths differ)
+        p.goal = 256 * (p.mt == 1 ? 3 : 2);
+        p.splits = tiles <= K8_MIN_TILES ? 1 : (int)std::min<int64_t>(K8_MAX_SPLITS, 2 + 2 * ((p.goal + units - 1) / units));
+        if (ws_bytes >= 0) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(p.splits, ws_bytes / one));
+        p.blocks = p.goal + units;
+    } else {
+        p.kernel = KV8_TILES, p.mt = 2;
+        const int64_t set = 64 * p.mt, goal = 512;
+        p.blocks = (rw.row_start ? a.total_rows * grps / set + rw.n : rw.n * ((R + set - 1) / set)) * c.kv_heads;
+        // a split takes K8_MIN_TILES tiles at least and the context K8_MAX_SPLITS splits at most
+        p.per = (int)std::max(std::max<int64_t>((tiles * p.blocks + goal - 1) / goal, (tiles + K8_MAX_SPLITS - 1) / K8_MAX_SPLITS), (int64_t)K8_MIN_TILES);
+        p.splits = (int)std::max<int64_t>(1, (tiles + p.per - 1) / p.per);
+        if (ws_bytes >= 0) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(p.splits, ws_bytes / one));
+    }
     return p;
 }
 
@@ -959,14 +1160,24 @@ int64_t kv8_attn_workspace(const Kv8View &c, const Kv8Rows &rw, const Kv8Attn &a
 template <int HD>
 static hipError_t mfma_launch(hipStream_t s, const Kv8Plan &p, const Kv8View &c, const Kv8Rows &rw, const Kv8Attn &a, float *part)
 {
-    if (p.blocks * c.kv_heads > 0x7fffffff / 256) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)(p.blocks * c.kv_heads), p.splits);
-#define STREAM(MT, T) hipLaunchKernelGGL((kv8_attn_stream_kernel<HD, MT, T>), grid, dim3(256), 0, s, c, rw, a, (int)(p.blocks / rw.n), p.splits, p.per, part)
-#define TILES(T) hipLaunchKernelGGL((kv8_attn_tile_kernel<HD, 2, T>), grid, dim3(256), 0, s, c, rw, a, p.splits, p.per, part)
+    if (p.blocks > 0x7fffffff / 256) return hipErrorInvalidValue;
     const bool bf16 = a.dtype == SD_BF16;
+    constexpr int NG = 1024 / HD; // rows that a block of a join has in hand
+#define STREAM(MT, T)                                                                                                                            \
+    do {                                                                                                                                         \
+        hipLaunchKernelGGL((kv8_attn_stream_kernel<HD, MT, T>), dim3((unsigned)p.blocks), dim3(256), 0, s, c, rw, a, p.splits, p.goal, part);      \
+        if (p.splits > 1) {                                                                                                                      \
+            const int groups = (int)((p.max_m + NG - 1) / NG);                                                                                   \
+            hipLaunchKernelGGL((kv8_attn_join_kernel<HD, 16 * MT>), dim3((unsigned)((int64_t)rw.n * c.kv_heads * groups)), dim3(256), 0, s, c, rw, a, \
+                               groups, p.splits, p.goal, part);                                                                                  \
+        }                                                                                                                                        \
+    } while (0)
+#define TILES(T) hipLaunchKernelGGL((kv8_attn_tile_kernel<HD, 2, T>), dim3((unsigned)p.blocks, p.splits), dim3(256), 0, s, c, rw, a, p.splits, p.per, part)
     if (p.kernel == KV8_TILES) {
         if (bf16) TILES(1);
         else TILES(2);
+        if (p.splits > 1)
+            hipLaunchKernelGGL(kv8_attn_join_tiles_kernel<HD>, dim3(a.total_rows, (a.n_heads + NG - 1) / NG), dim3(256), 0, s, c, rw, a, p.splits, p.per, part);
     } else if (p.mt == 1) {
         if (bf16) STREAM(1, 1);
         else STREAM(1, 2);
@@ -976,8 +1187,6 @@ static hipError_t mfma_launch(hipStream_t s, const Kv8Plan &p, const Kv8View &c,
     }
 #undef STREAM
 #undef TILES
-    if (p.splits > 1)
-        hipLaunchKernelGGL(kv8_attn_join_kernel<HD>, dim3(a.total_rows, a.n_heads), dim3(HD), 0, s, c, rw, a, p.set_rows, p.splits, p.per, part);
     return hipGetLastError();
 }
 

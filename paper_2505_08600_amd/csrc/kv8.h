@@ -32,6 +32,11 @@ struct Kv8Seq {
     int32_t row0, n_rows;
 };
 
+// Lengths and capacities are looked at up to 2^30, so that positions, a length and less than 2^30 more, are plain integers.
+#define KV8_MAX_TOKENS (1 << 30)
+__device__ __forceinline__ int kv8_length(int len) { return min(max(len, -KV8_MAX_TOKENS), KV8_MAX_TOKENS); }
+__device__ __forceinline__ int kv8_capacity(const Kv8View &c, int b) { return min(c.cap[b], KV8_MAX_TOKENS); }
+
 // uniform over the wave (every lane calls it)
 __device__ __forceinline__ Kv8Seq kv8_seq(const Kv8View &c, const Kv8Rows &rw, int j)
 {
@@ -40,7 +45,7 @@ __device__ __forceinline__ Kv8Seq kv8_seq(const Kv8View &c, const Kv8Rows &rw, i
     if (s.b < 0 || s.b >= c.n_seq) s.b = -1;
     s.row0 = rw.row_start ? rw.row_start[j] : j * rw.rows;
     s.n_rows = rw.row_start ? rw.row_start[j + 1] - s.row0 : rw.rows;
-    s.len = s.b < 0 ? 0 : rw.len[rw.path ? j * rw.group : s.b];
+    s.len = s.b < 0 ? 0 : kv8_length(rw.len[rw.path ? j * rw.group : s.b]);
     if (rw.path) {
         int t = 0;
         for (int g = threadIdx.x & 63; g < rw.group; g += 64) t += rw.nq[j * rw.group + g];

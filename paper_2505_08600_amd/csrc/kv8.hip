@@ -95,8 +95,8 @@ __device__ __forceinline__ int64_t row_place(const Kv8View &c, const Kv8Rows &rw
         if (flag && c.status) atomicOr(c.status, 4);
         return -1;
     }
-    const int64_t t = (int64_t)s.len + (r - s.row0);
-    if (t < 0 || t >= c.cap[s.b]) {
+    const int t = s.len + (r - s.row0);
+    if (t < 0 || t >= kv8_capacity(c, s.b)) {
         if (flag && c.status) atomicOr(c.status, 1);
         return -1;
     }
@@ -357,6 +357,8 @@ static int check_attn(const char *who, const sd_kv8 *c, const sd_kv8_attn *a)
     if (a->dtype != SD_FP32 && a->dtype != SD_BF16) return sd_fail(SD_EINVAL, std::string(who) + ": bad dtype");
     if (a->n_heads < 1 || a->n_heads > 65535 || a->n_heads % c->n_kv_heads)
         return sd_fail(SD_EINVAL, std::string(who) + ": n_heads must be a multiple of n_kv_heads");
+    if ((int64_t)a->rows * (a->n_heads / c->n_kv_heads) > 0x7fffffff)
+        return sd_fail(SD_EINVAL, std::string(who) + ": rows times query heads per cache head must fit 31 bits");
     if (a->max_rows < 0 || a->max_len < 0) return sd_fail(SD_EINVAL, std::string(who) + ": max_rows and max_len must not be negative");
     if (!std::isfinite(a->scale)) return sd_fail(SD_EINVAL, std::string(who) + ": scale must be finite");
     if (a->window < 0 || a->sinks < 0) return sd_fail(SD_EINVAL, std::string(who) + ": window and sinks must not be negative");
@@ -375,7 +377,7 @@ static Kv8Attn attn_of(const sd_kv8_attn *a)
     k.q = a->q, k.q_row = a->q_row, k.q_head = a->q_head;
     k.out = a->out, k.o_row = a->o_row, k.o_head = a->o_head;
     k.lse = a->lse, k.n_heads = a->n_heads, k.dtype = a->dtype;
-    k.causal = a->causal != 0, k.window = a->window, k.sinks = a->sinks;
+    k.causal = a->causal != 0, k.window = std::min(a->window, KV8_MAX_TOKENS), k.sinks = std::min(a->sinks, KV8_MAX_TOKENS);
     k.scale = a->scale * 1.44269504088896341f;
     k.total_rows = a->rows, k.max_len = a->max_len;
     k.max_rows = a->row_start ? a->max_rows : a->rows / a->n_seq;
