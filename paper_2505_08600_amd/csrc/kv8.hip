@@ -2,43 +2,59 @@
 //
 // A vector is one row of one head, K or V: scale = max|x| * (1 / 127), at least 2^-60, code = nearest integer to x / scale.
 // Bound of both kernels: memory.  D / 8 lanes hold a vector, 8 elements each: a 16-byte load (two for fp32), a maximum over the
-// lanes, an 8-byte store.  A block serves one row of the call, so that finding the row's sequence and place costs a block one
-// chain of small loads and not one per vector.
+// lanes, an 8-byte store.
 #include <cmath>
 
 #include <algorithm>
 
 #include "kv8.h"
 
+// The 8 elements that lane l of a vector holds: bf16 the adjacent ones from 8 l on; fp32 four from 4 l on and four from hd / 2 + 4 l on, so
+// that each access of the lanes together is one piece (8191 rows of 32 heads read back as fp32: 88 us with 8 adjacent, ... so).
 template <typename T, bool WIDE>
-__device__ __forceinline__ void load8(const T *p, float x[8])
+__device__ __forceinline__ void load8(const T *p, int l, int hd, float x[8])
 {
+    const int d0 = sizeof(T) == 2 ? 8 * l : 4 * l, d1 = sizeof(T) == 2 ? d0 + 4 : hd / 2 + d0;
     if constexpr (WIDE && sizeof(T) == 2) {
-        const uint4 w = *(const uint4 *)p;
+        const uint4 w = *(const uint4 *)(p + d0);
         const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
         for (int e = 0; e < 4; e++) x[2 * e] = __uint_as_float(u[e] << 16), x[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
     } else if constexpr (WIDE) {
-        const float4 a = *(const float4 *)p, b = *(const float4 *)(p + 4);
+        const float4 a = *(const float4 *)(p + d0), b = *(const float4 *)(p + d1);
         x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; e++) x[e] = to_float(p[e]);
+        for (int e = 0; e < 4; e++) x[e] = to_float(p[d0 + e]), x[4 + e] = to_float(p[d1 + e]);
     }
 }
 
 template <typename T, bool WIDE>
-__device__ __forceinline__ void store8(T *p, const float x[8])
+__device__ __forceinline__ void store8(T *p, int l, int hd, const float x[8])
 {
+    const int d0 = sizeof(T) == 2 ? 8 * l : 4 * l, d1 = sizeof(T) == 2 ? d0 + 4 : hd / 2 + d0;
     if constexpr (WIDE && sizeof(T) == 2) {
-        *(uint4 *)p = make_uint4(bf16x2_bits_rne(x[0], x[1]), bf16x2_bits_rne(x[2], x[3]), bf16x2_bits_rne(x[4], x[5]), bf16x2_bits_rne(x[6], x[7]));
+        *(uint4 *)(p + d0) = make_uint4(bf16x2_bits_rne(x[0], x[1]), bf16x2_bits_rne(x[2], x[3]), bf16x2_bits_rne(x[4], x[5]), bf16x2_bits_rne(x[6], x[7]));
     } else if constexpr (WIDE) {
-        *(float4 *)p = make_float4(x[0], x[1], x[2], x[3]);
-        *(float4 *)(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+        *(float4 *)(p + d0) = make_float4(x[0], x[1], x[2], x[3]);
+        *(float4 *)(p + d1) = make_float4(x[4], x[5], x[6], x[7]);
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; e++) p[e] = from_float<T>(x[e]);
+        for (int e = 0; e < 4; e++) p[d0 + e] = from_float<T>(x[e]), p[d1 + e] = from_float<T>(x[4 + e]);
     }
+}
+// ... and their codes
+template <typename T>
+__device__ __forceinline__ uint2 load_codes(const int8_t *p, int l, int hd)
+{
+    if constexpr (sizeof(T) == 2) return *(const uint2 *)(p + 8 * l);
+    else return make_uint2(*(const uint32_t *)(p + 4 * l), *(const uint32_t *)(p + hd / 2 + 4 * l));
+}
+template <typename T>
+__device__ __forceinline__ void store_codes(int8_t *p, int l, int hd, uint2 u)
+{
+    if constexpr (sizeof(T) == 2) *(uint2 *)(p + 8 * l) = u;
+    else *(uint32_t *)(p + 4 * l) = u.x, *(uint32_t *)(p + hd / 2 + 4 * l) = u.y;
 }
 
 // Largest magnitude of 8 elements as bits (a NaN's are above infinity's, which are above every finite value's) ...
@@ -85,125 +101,169 @@ __device__ __forceinline__ void dequantise4(uint32_t u, float s, float x[4])
     for (int e = 0; e < 4; e++) x[e] = (float)((int32_t)(u << (24 - 8 * e)) >> 24) * s;
 }
 
-// Place of row r: its cache row in every head, or -1 (none: not a row of the call, or outside its sequence).
+// Place of row r: its cache row in every head, or -1 (none: not a row of the call, or outside its sequence).  Each thread for a row of its
+// own.
 __device__ __forceinline__ int64_t row_place(const Kv8View &c, const Kv8Rows &rw, int r, bool flag)
 {
-    const int j = kv8_owner(rw, r);
-    if (j < 0 || j >= rw.n) return -1;
-    const Kv8Seq s = kv8_seq(c, rw, j);
-    if (s.b < 0) {
+    int j, first;
+    if (rw.row_start) { // the last sequence whose first row is not behind r
+        int lo = 0, hi = rw.n;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) / 2;
+            if (rw.row_start[mid] <= r) lo = mid;
+            else hi = mid - 1;
+        }
+        j = lo, first = rw.row_start[j];
+        if (j == rw.n || first > r) return -1;
+    } else j = (unsigned)r / (unsigned)rw.rows, first = j * rw.rows;
+    const int b = rw.seq_ids ? rw.seq_ids[j] : j;
+    if (b < 0 || b >= c.n_seq) {
         if (flag && c.status) atomicOr(c.status, 4);
         return -1;
     }
-    const int t = s.len + (r - s.row0);
-    if (t < 0 || t >= kv8_capacity(c, s.b)) {
+    const int t = kv8_length(rw.len[b]) + (r - first);
+    if (t < 0 || t >= kv8_capacity(c, b)) {
         if (flag && c.status) atomicOr(c.status, 1);
         return -1;
     }
-    return c.off[s.b] + t;
+    return c.off[b] + t;
 }
 
-template <typename T, bool WIDE>
-__global__ __launch_bounds__(256) void kv8_append_kernel(Kv8View c, Kv8Rows rw, int lanes, const T *__restrict__ k, int64_t k_row, int64_t k_head,
-                                                         const T *__restrict__ v, int64_t v_row, int64_t v_head)
+// Both kernels: a block serves RB adjacent rows.  Its first threads find the rows' places; pieces of 8 elements are then dealt out with a
+// vector's lanes innermost, then the rows, then the vectors (K and V of each head), so that the codes of adjacent tokens are
+// touched together, and four at a time per thread, so that their loads are in flight together.
+template <int RB>
+struct Kv8Piece {
+    int l, row, w; // lane of the vector, row of the block, vector (2 * head + (0: K, 1: V))
+};
+template <int RB>
+__device__ __forceinline__ Kv8Piece<RB> kv8_piece(int u, int lane_bits)
 {
-    const int r = blockIdx.x;
-    const int64_t at = row_place(c, rw, r, threadIdx.x == 0 && blockIdx.y == 0);
-    if (at < 0) return;
-    const int per_block = 256 / lanes, l = threadIdx.x & (lanes - 1);
-    const bool mine = l * 8 < c.hd;
-    for (int u = blockIdx.y * per_block; u < 2 * c.kv_heads; u += gridDim.y * per_block) { // (the same count for every lane: shuffles)
-        const int w = min(u + (int)threadIdx.x / lanes, 2 * c.kv_heads - 1);
-        const int h = w >> 1;
-        const T *src = w & 1 ? v + r * v_row + h * v_head : k + r * k_row + h * k_head;
-        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (mine) load8<T, WIDE>(src + 8 * l, x);
-        const float s = kv8_scale(amax_lanes(amax_bits8(x), lanes)), inv = 1.0f / s;
-        const bool fine = s == s;
-        if (u + (int)threadIdx.x / lanes >= 2 * c.kv_heads || !mine) continue;
-        const int64_t row = (int64_t)h * c.tokens + at;
-        const uint2 codes = fine ? make_uint2(quantise4(x, s, inv), quantise4(x + 4, s, inv)) : make_uint2(0, 0);
-        *(uint2 *)((w & 1 ? c.v : c.k) + row * c.hd + 8 * l) = codes;
-        if (l == 0) (w & 1 ? c.vs : c.ks)[row] = s;
+    return Kv8Piece<RB>{u & ((1 << lane_bits) - 1), (u >> lane_bits) % RB, (u >> lane_bits) / RB};
+}
+
+template <typename T, bool WIDE, int RB>
+__global__ __launch_bounds__(256) void kv8_append_kernel(Kv8View c, Kv8Rows rw, int n_rows, int lane_bits, const T *__restrict__ k, int64_t k_row,
+                                                         int64_t k_head, const T *__restrict__ v, int64_t v_row, int64_t v_head)
+{
+    __shared__ int64_t s_at[RB];
+    const int r0 = blockIdx.x * RB;
+    if (threadIdx.x < RB) s_at[threadIdx.x] = r0 + (int)threadIdx.x < n_rows ? row_place(c, rw, r0 + threadIdx.x, blockIdx.y == 0) : -1;
+    __syncthreads();
+    const int n = (2 * c.kv_heads * RB) << lane_bits, lanes = 1 << lane_bits;
+    for (int u0 = blockIdx.y * 1024; u0 < n; u0 += gridDim.y * 1024) { // (the same count for every lane: shuffles)
+        float x[4][8];
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+#pragma unroll
+            for (int e = 0; e < 8; e++) x[q][e] = 0.f;
+            const int u = u0 + 256 * q + threadIdx.x;
+            const Kv8Piece<RB> p = kv8_piece<RB>(u, lane_bits);
+            if (u >= n || p.l * 8 >= c.hd || s_at[p.row] < 0) continue;
+            const int64_t r = r0 + p.row;
+            const int h = p.w >> 1;
+            load8<T, WIDE>(p.w & 1 ? v + r * v_row + h * v_head : k + r * k_row + h * k_head, p.l, c.hd, x[q]);
+        }
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+            const int u = u0 + 256 * q + threadIdx.x;
+            const Kv8Piece<RB> p = kv8_piece<RB>(u, lane_bits);
+            const float s = kv8_scale(amax_lanes(amax_bits8(x[q]), lanes)), inv = 1.0f / s;
+            if (u >= n || p.l * 8 >= c.hd || s_at[p.row] < 0) continue;
+            const int64_t row = (int64_t)(p.w >> 1) * c.tokens + s_at[p.row];
+            const uint2 codes = s == s ? make_uint2(quantise4(x[q], s, inv), quantise4(x[q] + 4, s, inv)) : make_uint2(0, 0);
+            store_codes<T>((p.w & 1 ? c.v : c.k) + row * c.hd, p.l, c.hd, codes);
+            if (p.l == 0) (p.w & 1 ? c.vs : c.ks)[row] = s;
+        }
     }
 }
 
-template <typename T, bool WIDE>
-__global__ __launch_bounds__(256) void kv8_read_kernel(Kv8View c, Kv8Rows rw, int lanes, T *__restrict__ k, int64_t k_row, int64_t k_head,
-                                                       T *__restrict__ v, int64_t v_row, int64_t v_head)
+template <typename T, bool WIDE, int RB>
+__global__ __launch_bounds__(256) void kv8_read_kernel(Kv8View c, Kv8Rows rw, int n_rows, int lane_bits, T *__restrict__ k, int64_t k_row,
+                                                       int64_t k_head, T *__restrict__ v, int64_t v_row, int64_t v_head)
 {
-    const int r = blockIdx.x;
-    const int64_t at = row_place(c, rw, r, threadIdx.x == 0 && blockIdx.y == 0);
-    if (at < 0) return;
-    const int per_block = 256 / lanes, l = threadIdx.x & (lanes - 1);
-    if (l * 8 >= c.hd) return;
-    for (int w = blockIdx.y * per_block + threadIdx.x / lanes; w < 2 * c.kv_heads; w += gridDim.y * per_block) {
-        const int h = w >> 1;
-        T *dst = w & 1 ? v : k;
-        if (!dst) continue;
-        dst += w & 1 ? r * v_row + h * v_head : r * k_row + h * k_head;
-        const int64_t row = (int64_t)h * c.tokens + at;
-        const uint2 u = *(const uint2 *)((w & 1 ? c.v : c.k) + row * c.hd + 8 * l);
-        const float s = (w & 1 ? c.vs : c.ks)[row];
-        float x[8];
-        dequantise4(u.x, s, x);
-        dequantise4(u.y, s, x + 4);
-        store8<T, WIDE>(dst + 8 * l, x);
+    __shared__ int64_t s_at[RB];
+    const int r0 = blockIdx.x * RB;
+    if (threadIdx.x < RB) s_at[threadIdx.x] = r0 + (int)threadIdx.x < n_rows ? row_place(c, rw, r0 + threadIdx.x, blockIdx.y == 0) : -1;
+    __syncthreads();
+    const int n = (2 * c.kv_heads * RB) << lane_bits;
+    for (int u0 = blockIdx.y * 1024; u0 < n; u0 += gridDim.y * 1024) {
+        uint2 w[4];
+        float s[4];
+        bool live[4];
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+            const int u = u0 + 256 * q + threadIdx.x;
+            const Kv8Piece<RB> p = kv8_piece<RB>(u, lane_bits);
+            live[q] = u < n && p.l * 8 < c.hd && s_at[p.row] >= 0 && (p.w & 1 ? v : k);
+            if (!live[q]) continue;
+            const int64_t row = (int64_t)(p.w >> 1) * c.tokens + s_at[p.row];
+            w[q] = load_codes<T>((p.w & 1 ? c.v : c.k) + row * c.hd, p.l, c.hd);
+            s[q] = (p.w & 1 ? c.vs : c.ks)[row];
+        }
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+            if (!live[q]) continue;
+            const Kv8Piece<RB> p = kv8_piece<RB>(u0 + 256 * q + threadIdx.x, lane_bits);
+            const int64_t r = r0 + p.row;
+            const int h = p.w >> 1;
+            float x[8];
+            dequantise4(w[q].x, s[q], x);
+            dequantise4(w[q].y, s[q], x + 4);
+            store8<T, WIDE>(p.w & 1 ? v + r * v_row + h * v_head : k + r * k_row + h * k_head, p.l, c.hd, x);
+        }
     }
 }
 
 // lanes of a vector: the power of two that holds head_dim / 8
-static int vector_lanes(int hd)
+static int vector_lane_bits(int hd)
 {
-    int l = 2;
-    while (l * 8 < hd) l *= 2;
-    return l;
+    int b = 1;
+    while ((8 << b) < hd) b++;
+    return b;
 }
 static bool wide_rows(int esz, const void *p, int64_t row, int64_t head)
 {
     return ((uintptr_t)p % 16) == 0 && row * esz % 16 == 0 && head * esz % 16 == 0;
 }
-// few rows: one pass per block, so that the vectors of a row spread over the compute units; many: a row per block
-static dim3 vector_grid(int n_rows, int kv_heads, int lanes)
+// Few rows: a row per block, and its vectors spread over blocks too, so that the chip fills; many: eight rows per block, so that a
+// block's search for its rows is paid for by more bytes (51200 rows of 8 heads of 128, bf16: 92 us with one row, ... with eight).
+#define KV8_ROWS 8
+static dim3 vector_grid(int n_rows, int rb, int kv_heads, int lane_bits)
 {
-    const int passes = (2 * kv_heads * lanes + 255) / 256;
-    return dim3(n_rows, std::max(1, std::min(passes, 2048 / n_rows)));
+    const int gx = (n_rows + rb - 1) / rb, turns = ((2 * kv_heads * rb << lane_bits) + 1023) / 1024;
+    return dim3(gx, std::max(1, std::min(turns, 2048 / gx)));
 }
+
+#define KV8_MOVE(KERNEL, CV)                                                                                                                   \
+    const int esz = dtype == SD_BF16 ? 2 : 4, bits = vector_lane_bits(c.hd), rb = n_rows >= 2048 ? KV8_ROWS : 1;                               \
+    const bool wide = wide_rows(esz, k, k_row, k_head) && wide_rows(esz, v, v_row, v_head); /* (a null pointer counts as aligned) */            \
+    const dim3 grid = vector_grid(n_rows, rb, c.kv_heads, bits);                                                                               \
+    if (dtype == SD_BF16) {                                                                                                                    \
+        if (wide && rb > 1) KV8_GO(KERNEL, CV bf16_t, bf16_t, true, KV8_ROWS);                                                                 \
+        else if (wide) KV8_GO(KERNEL, CV bf16_t, bf16_t, true, 1);                                                                             \
+        else if (rb > 1) KV8_GO(KERNEL, CV bf16_t, bf16_t, false, KV8_ROWS);                                                                   \
+        else KV8_GO(KERNEL, CV bf16_t, bf16_t, false, 1);                                                                                      \
+    } else {                                                                                                                                   \
+        if (wide && rb > 1) KV8_GO(KERNEL, CV float, float, true, KV8_ROWS);                                                                   \
+        else if (wide) KV8_GO(KERNEL, CV float, float, true, 1);                                                                               \
+        else if (rb > 1) KV8_GO(KERNEL, CV float, float, false, KV8_ROWS);                                                                     \
+        else KV8_GO(KERNEL, CV float, float, false, 1);                                                                                        \
+    }                                                                                                                                          \
+    return hipGetLastError();
+#define KV8_GO(KERNEL, P, T, W, RB) \
+    hipLaunchKernelGGL((KERNEL<T, W, RB>), grid, dim3(256), 0, s, c, rw, n_rows, bits, (P *)k, k_row, k_head, (P *)v, v_row, v_head)
 
 hipError_t launch_kv8_append(hipStream_t s, const Kv8View &c, const Kv8Rows &rw, int n_rows, int dtype, const void *k, int64_t k_row,
                              int64_t k_head, const void *v, int64_t v_row, int64_t v_head)
 {
-    const int esz = dtype == SD_BF16 ? 2 : 4, lanes = vector_lanes(c.hd);
-    const bool wide = wide_rows(esz, k, k_row, k_head) && wide_rows(esz, v, v_row, v_head);
-    const dim3 grid = vector_grid(n_rows, c.kv_heads, lanes);
-#define GO(T, W) hipLaunchKernelGGL((kv8_append_kernel<T, W>), grid, dim3(256), 0, s, c, rw, lanes, (const T *)k, k_row, k_head, (const T *)v, v_row, v_head)
-    if (dtype == SD_BF16) {
-        if (wide) GO(bf16_t, true);
-        else GO(bf16_t, false);
-    } else {
-        if (wide) GO(float, true);
-        else GO(float, false);
-    }
-#undef GO
-    return hipGetLastError();
+    KV8_MOVE(kv8_append_kernel, const)
 }
 
 hipError_t launch_kv8_read(hipStream_t s, const Kv8View &c, const Kv8Rows &rw, int n_rows, int dtype, void *k, int64_t k_row, int64_t k_head,
                            void *v, int64_t v_row, int64_t v_head)
 {
-    const int esz = dtype == SD_BF16 ? 2 : 4, lanes = vector_lanes(c.hd);
-    const bool wide = wide_rows(esz, k, k_row, k_head) && wide_rows(esz, v, v_row, v_head); // (a null pointer counts as aligned)
-    const dim3 grid = vector_grid(n_rows, c.kv_heads, lanes);
-#define GO(T, W) hipLaunchKernelGGL((kv8_read_kernel<T, W>), grid, dim3(256), 0, s, c, rw, lanes, (T *)k, k_row, k_head, (T *)v, v_row, v_head)
-    if (dtype == SD_BF16) {
-        if (wide) GO(bf16_t, true);
-        else GO(bf16_t, false);
-    } else {
-        if (wide) GO(float, true);
-        else GO(float, false);
-    }
-#undef GO
-    return hipGetLastError();
+    KV8_MOVE(kv8_read_kernel, )
 }
 
 // ---------------------------------------------------------------- the path's step between projection and attention
