@@ -10,18 +10,26 @@
 #include "kv8.h"
 
 // The 8 elements that lane l of a vector holds: bf16 the adjacent ones from 8 l on; fp32 four from 4 l on and four from hd / 2 + 4 l on, so
-// that each access of the lanes together is one piece (8191 rows of 32 heads read back as fp32: 88 us with 8 adjacent, ... so).
-template <typename T, bool WIDE>
+// that each access of the lanes together is one piece (8191 rows of 32 heads read back as fp32: 88 us with 8 adjacent, 68 so).
+// NT: with the nontemporal hint, for what is read or written once and is much (8191 fp32 rows of 32 heads into the cache: 99 us without,
+// 80 with the loads, 64 with loads and stores; back out of it 70, 70, 65).
+template <bool NT, typename V>
+__device__ __forceinline__ V load_v(const void *p)
+{
+    typedef __attribute__((ext_vector_type(sizeof(V) / 4))) uint32_t words;
+    return __builtin_bit_cast(V, ld_stream<NT>((const words *)p));
+}
+template <typename T, bool WIDE, bool NT>
 __device__ __forceinline__ void load8(const T *p, int l, int hd, float x[8])
 {
     const int d0 = sizeof(T) == 2 ? 8 * l : 4 * l, d1 = sizeof(T) == 2 ? d0 + 4 : hd / 2 + d0;
     if constexpr (WIDE && sizeof(T) == 2) {
-        const uint4 w = *(const uint4 *)(p + d0);
+        const uint4 w = load_v<NT, uint4>(p + d0);
         const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
         for (int e = 0; e < 4; e++) x[2 * e] = __uint_as_float(u[e] << 16), x[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
     } else if constexpr (WIDE) {
-        const float4 a = *(const float4 *)(p + d0), b = *(const float4 *)(p + d1);
+        const float4 a = load_v<NT, float4>(p + d0), b = load_v<NT, float4>(p + d1);
         x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
     } else {
 #pragma unroll
@@ -29,26 +37,33 @@ __device__ __forceinline__ void load8(const T *p, int l, int hd, float x[8])
     }
 }
 
-template <typename T, bool WIDE>
+template <bool NT, typename V>
+__device__ __forceinline__ void store_v(void *p, V v)
+{
+    typedef __attribute__((ext_vector_type(sizeof(V) / 4))) uint32_t words;
+    if constexpr (NT) __builtin_nontemporal_store(__builtin_bit_cast(words, v), (words *)p);
+    else *(V *)p = v;
+}
+template <typename T, bool WIDE, bool NT>
 __device__ __forceinline__ void store8(T *p, int l, int hd, const float x[8])
 {
     const int d0 = sizeof(T) == 2 ? 8 * l : 4 * l, d1 = sizeof(T) == 2 ? d0 + 4 : hd / 2 + d0;
     if constexpr (WIDE && sizeof(T) == 2) {
-        *(uint4 *)(p + d0) = make_uint4(bf16x2_bits_rne(x[0], x[1]), bf16x2_bits_rne(x[2], x[3]), bf16x2_bits_rne(x[4], x[5]), bf16x2_bits_rne(x[6], x[7]));
+        store_v<NT>(p + d0, make_uint4(bf16x2_bits_rne(x[0], x[1]), bf16x2_bits_rne(x[2], x[3]), bf16x2_bits_rne(x[4], x[5]), bf16x2_bits_rne(x[6], x[7])));
     } else if constexpr (WIDE) {
-        *(float4 *)(p + d0) = make_float4(x[0], x[1], x[2], x[3]);
-        *(float4 *)(p + d1) = make_float4(x[4], x[5], x[6], x[7]);
+        store_v<NT>(p + d0, make_float4(x[0], x[1], x[2], x[3]));
+        store_v<NT>(p + d1, make_float4(x[4], x[5], x[6], x[7]));
     } else {
 #pragma unroll
         for (int e = 0; e < 4; e++) p[d0 + e] = from_float<T>(x[e]), p[d1 + e] = from_float<T>(x[4 + e]);
     }
 }
 // ... and their codes
-template <typename T>
+template <typename T, bool NT>
 __device__ __forceinline__ uint2 load_codes(const int8_t *p, int l, int hd)
 {
-    if constexpr (sizeof(T) == 2) return *(const uint2 *)(p + 8 * l);
-    else return make_uint2(*(const uint32_t *)(p + 4 * l), *(const uint32_t *)(p + hd / 2 + 4 * l));
+    if constexpr (sizeof(T) == 2) return load_v<NT, uint2>(p + 8 * l);
+    else return make_uint2(ld_stream<NT>((const uint32_t *)(p + 4 * l)), ld_stream<NT>((const uint32_t *)(p + hd / 2 + 4 * l)));
 }
 template <typename T>
 __device__ __forceinline__ void store_codes(int8_t *p, int l, int hd, uint2 u)
@@ -65,10 +80,17 @@ __device__ __forceinline__ uint32_t amax_bits8(const float x[8])
     for (int e = 0; e < 8; e++) m = max(m, __float_as_uint(x[e]) & 0x7fffffffu);
     return m;
 }
-// ... over the `width` (a power of two) lanes of a vector ...
-__device__ __forceinline__ uint32_t amax_lanes(uint32_t m, int width)
+// ... over the 2^bits adjacent lanes of a vector, left in each of them (the exchanges stay inside a row of 16 lanes but the last) ...
+__device__ __forceinline__ uint32_t amax_lanes(uint32_t m, int bits)
 {
-    for (int o = 1; o < width; o <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
+    m = max(m, (uint32_t)dpp_i<0xB1>((int)m));
+    if (bits > 1) m = max(m, (uint32_t)dpp_i<0x4E>((int)m));
+    if (bits > 2) m = max(m, (uint32_t)dpp_i<0x141>((int)m));
+    if (bits > 3) m = max(m, (uint32_t)dpp_i<0x140>((int)m));
+    if (bits > 4) {
+        const auto s = __builtin_amdgcn_permlane16_swap(m, m, false, false);
+        m = max(s[0], s[1]);
+    }
     return m;
 }
 // ... and the scale it gives: NaN where the vector holds a NaN or an infinity.
@@ -80,19 +102,36 @@ __device__ __forceinline__ float kv8_scale(uint32_t amax)
 // The integer nearest to x / s, ties to even.  x * (1 / s) is off by a few parts in 2^24, so its rounding can end on the wrong
 // side of a half; e = x - q s is exact (a multiple of the coarser of the two last places, and no larger than s), so comparing it
 // with s / 2 settles the case.
-__device__ __forceinline__ int quantise(float x, float s, float inv)
+__device__ __forceinline__ uint32_t quantise(float x, float s, float inv)
 {
     const float q = rintf(x * inv), e = fmaf(-q, s, x), half = 0.5f * s;
-    int c = (int)q;
+    const int c = (int)q;
     const bool over = fabsf(e) > half || (fabsf(e) == half && (c & 1));
-    return over ? c + (e > 0.f ? 1 : -1) : c;
+    return (uint32_t)(over ? c + (e > 0.f ? 1 : -1) : c) & 255u;
 }
-__device__ __forceinline__ uint32_t quantise4(const float x[4], float s, float inv)
+// Eight of them.  1.5 * 2^23 + x / s, rounded once, has the integer in its low byte; only where some |e| reaches s / 2 is there
+// anything to settle (30 vector operations an element done singly, 7 so).
+__device__ __forceinline__ uint2 quantise8(const float x[8], float s, float inv)
 {
-    uint32_t u = 0;
+    uint32_t t[8];
+    float e[8];
 #pragma unroll
-    for (int e = 0; e < 4; e++) u |= ((uint32_t)quantise(x[e], s, inv) & 255u) << (8 * e);
-    return u;
+    for (int i = 0; i < 8; i++) {
+        const float f = fmaf(x[i], inv, 12582912.f);
+        t[i] = __float_as_uint(f);
+        e[i] = fmaf(12582912.f - f, s, x[i]);
+    }
+    float m = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; i++) m = fmaxf(m, fabsf(e[i]));
+    if (__any(m >= 0.5f * s)) {
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < 8; i++) t[i] = quantise(x[i], s, inv);
+    }
+    const uint32_t a = __builtin_amdgcn_perm(t[1], t[0], 0x0c0c0400u), b = __builtin_amdgcn_perm(t[3], t[2], 0x04000c0cu);
+    const uint32_t c = __builtin_amdgcn_perm(t[5], t[4], 0x0c0c0400u), d = __builtin_amdgcn_perm(t[7], t[6], 0x04000c0cu);
+    return make_uint2(a | b, c | d);
 }
 // codes of four bytes, as values
 __device__ __forceinline__ void dequantise4(uint32_t u, float s, float x[4])
@@ -129,7 +168,7 @@ __device__ __forceinline__ int64_t row_place(const Kv8View &c, const Kv8Rows &rw
     return c.off[b] + t;
 }
 
-// Both kernels: a block serves RB adjacent rows.  Its first threads find the rows' places; pieces of 8 elements are then dealt out with a
+// Both kernels: a block serves RB adjacent rows (RB > 1: and memory with the nontemporal hint).  Its first threads find the rows' places; pieces of 8 elements are then dealt out with a
 // vector's lanes innermost, then the rows, then the vectors (K and V of each head), so that the codes of adjacent tokens are
 // touched together, and four at a time per thread, so that their loads are in flight together.
 template <int RB>
@@ -150,7 +189,7 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8View c, Kv8Rows rw, 
     const int r0 = blockIdx.x * RB;
     if (threadIdx.x < RB) s_at[threadIdx.x] = r0 + (int)threadIdx.x < n_rows ? row_place(c, rw, r0 + threadIdx.x, blockIdx.y == 0) : -1;
     __syncthreads();
-    const int n = (2 * c.kv_heads * RB) << lane_bits, lanes = 1 << lane_bits;
+    const int n = (2 * c.kv_heads * RB) << lane_bits;
     for (int u0 = blockIdx.y * 1024; u0 < n; u0 += gridDim.y * 1024) { // (the same count for every lane: shuffles)
         float x[4][8];
 #pragma unroll
@@ -162,16 +201,16 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8View c, Kv8Rows rw, 
             if (u >= n || p.l * 8 >= c.hd || s_at[p.row] < 0) continue;
             const int64_t r = r0 + p.row;
             const int h = p.w >> 1;
-            load8<T, WIDE>(p.w & 1 ? v + r * v_row + h * v_head : k + r * k_row + h * k_head, p.l, c.hd, x[q]);
+            load8<T, WIDE, (RB > 1)>(p.w & 1 ? v + r * v_row + h * v_head : k + r * k_row + h * k_head, p.l, c.hd, x[q]);
         }
 #pragma unroll
         for (int q = 0; q < 4; q++) {
             const int u = u0 + 256 * q + threadIdx.x;
             const Kv8Piece<RB> p = kv8_piece<RB>(u, lane_bits);
-            const float s = kv8_scale(amax_lanes(amax_bits8(x[q]), lanes)), inv = 1.0f / s;
+            const float s = kv8_scale(amax_lanes(amax_bits8(x[q]), lane_bits)), inv = 1.0f / s;
             if (u >= n || p.l * 8 >= c.hd || s_at[p.row] < 0) continue;
             const int64_t row = (int64_t)(p.w >> 1) * c.tokens + s_at[p.row];
-            const uint2 codes = s == s ? make_uint2(quantise4(x[q], s, inv), quantise4(x[q] + 4, s, inv)) : make_uint2(0, 0);
+            const uint2 codes = s == s ? quantise8(x[q], s, inv) : make_uint2(0, 0);
             store_codes<T>((p.w & 1 ? c.v : c.k) + row * c.hd, p.l, c.hd, codes);
             if (p.l == 0) (p.w & 1 ? c.vs : c.ks)[row] = s;
         }
@@ -198,7 +237,7 @@ __global__ __launch_bounds__(256) void kv8_read_kernel(Kv8View c, Kv8Rows rw, in
             live[q] = u < n && p.l * 8 < c.hd && s_at[p.row] >= 0 && (p.w & 1 ? v : k);
             if (!live[q]) continue;
             const int64_t row = (int64_t)(p.w >> 1) * c.tokens + s_at[p.row];
-            w[q] = load_codes<T>((p.w & 1 ? c.v : c.k) + row * c.hd, p.l, c.hd);
+            w[q] = load_codes<T, (RB > 1)>((p.w & 1 ? c.v : c.k) + row * c.hd, p.l, c.hd);
             s[q] = (p.w & 1 ? c.vs : c.ks)[row];
         }
 #pragma unroll
@@ -210,7 +249,7 @@ __global__ __launch_bounds__(256) void kv8_read_kernel(Kv8View c, Kv8Rows rw, in
             float x[8];
             dequantise4(w[q].x, s[q], x);
             dequantise4(w[q].y, s[q], x + 4);
-            store8<T, WIDE>(p.w & 1 ? v + r * v_row + h * v_head : k + r * k_row + h * k_head, p.l, c.hd, x);
+            store8<T, WIDE, (RB > 1)>(p.w & 1 ? v + r * v_row + h * v_head : k + r * k_row + h * k_head, p.l, c.hd, x);
         }
     }
 }
@@ -226,9 +265,10 @@ static bool wide_rows(int esz, const void *p, int64_t row, int64_t head)
 {
     return ((uintptr_t)p % 16) == 0 && row * esz % 16 == 0 && head * esz % 16 == 0;
 }
-// Few rows: a row per block, and its vectors spread over blocks too, so that the chip fills; many: eight rows per block, so that a
-// block's search for its rows is paid for by more bytes (51200 rows of 8 heads of 128, bf16: 92 us with one row, ... with eight).
-#define KV8_ROWS 8
+// Few rows: a row per block, and its vectors spread over blocks too, so that the chip fills; many: 32 rows per block, so that a
+// block's search for its rows is paid for by more bytes (51200 rows of 8 heads of 128 read back as bf16: 92 us with one row, 77 with
+// 8 to 64).
+#define KV8_ROWS 32
 static dim3 vector_grid(int n_rows, int rb, int kv_heads, int lane_bits)
 {
     const int gx = (n_rows + rb - 1) / rb, turns = ((2 * kv_heads * rb << lane_bits) + 1023) / 1024;
@@ -270,7 +310,7 @@ hipError_t launch_kv8_read(hipStream_t s, const Kv8View &c, const Kv8Rows &rw, i
 // hd / 8 lanes per vector as above, but a lane holds four dimensions of each rotary half, so that a pair never crosses lanes.
 #define KV8_MAX_SLABS 8
 __global__ __launch_bounds__(256) void kv8_rope_append_kernel(const float *__restrict__ qkv, int n_slabs, size_t slab_stride, PlanView pv,
-                                                              CtxView cv, Kv8View c, int lanes, int H, const float2 *__restrict__ rope, int max_pos,
+                                                              CtxView cv, Kv8View c, int lane_bits, int H, const float2 *__restrict__ rope, int max_pos,
                                                               float *__restrict__ q, int first)
 {
     const int r = blockIdx.x, hd = c.hd, half = hd / 2, HD = H * hd;
@@ -281,7 +321,7 @@ __global__ __launch_bounds__(256) void kv8_rope_append_kernel(const float *__res
         valid = false;
     }
     const int64_t at = cv.off[pv.row_b[r]] + pos;
-    const int per_block = 256 / lanes, l = threadIdx.x & (lanes - 1), d0 = 4 * l, d1 = half + 4 * l;
+    const int lanes = 1 << lane_bits, per_block = 256 / lanes, l = threadIdx.x & (lanes - 1), d0 = 4 * l, d1 = half + 4 * l;
     // vectors: the H heads of q (unless first = 1: the rows hold keys and values only), of k, of v
     const int n = (3 - first) * H;
     const float *row = qkv + (size_t)r * n * hd;
@@ -311,13 +351,14 @@ __global__ __launch_bounds__(256) void kv8_rope_append_kernel(const float *__res
                 *(float4 *)(dst + d1) = make_float4(x[4], x[5], x[6], x[7]);
             }
         }
-        const float s = kv8_scale(amax_lanes(amax_bits8(x), lanes)), inv = 1.0f / s; // (every lane takes part)
+        const float s = kv8_scale(amax_lanes(amax_bits8(x), lane_bits)), inv = 1.0f / s; // (every lane takes part)
         if (!valid || !live || part == 0) continue;
         const bool fine = s == s;
         const int64_t i = (int64_t)h * c.tokens + at;
         int8_t *dst = (part == 2 ? c.v : c.k) + i * hd;
-        *(uint32_t *)(dst + d0) = fine ? quantise4(x, s, inv) : 0u;
-        *(uint32_t *)(dst + d1) = fine ? quantise4(x + 4, s, inv) : 0u;
+        const uint2 codes = fine ? quantise8(x, s, inv) : make_uint2(0, 0);
+        *(uint32_t *)(dst + d0) = codes.x;
+        *(uint32_t *)(dst + d1) = codes.y;
         if (l == 0) (part == 2 ? c.vs : c.ks)[i] = s;
     }
 }
@@ -328,7 +369,7 @@ hipError_t launch_kv8_rope_append(hipStream_t s, const float *qkv, int n_slabs, 
     if (n_slabs > KV8_MAX_SLABS || c.hd < 16 || c.hd > 128 || (c.hd & (c.hd - 1))) return hipErrorInvalidValue; // (the path's head widths: powers of two)
     const int lanes = c.hd / 8, first = kv_only ? 1 : 0, passes = ((3 - first) * H * lanes + 255) / 256;
     const dim3 grid(M, std::max(1, std::min(passes, 2048 / M)));
-    hipLaunchKernelGGL(kv8_rope_append_kernel, grid, dim3(256), 0, s, qkv, n_slabs, slab_stride, pv, cv, c, lanes, H, rope, max_pos, q, first);
+    hipLaunchKernelGGL(kv8_rope_append_kernel, grid, dim3(256), 0, s, qkv, n_slabs, slab_stride, pv, cv, c, vector_lane_bits(c.hd), H, rope, max_pos, q, first);
     return hipGetLastError();
 }
 
