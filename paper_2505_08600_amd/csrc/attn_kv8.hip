@@ -860,28 +860,30 @@ __global__ __launch_bounds__(256, 3) void kv8_attn_tile_kernel(Kv8View c, Kv8Row
     float ss = 0.f;
     // (byte offsets inside a tile)
     const uint32_t stage_at = wave < 2 ? (16 * wave + qi) * HD + 16 * grp : 4 * grp * HD + VB * qi + (HD == 128 ? 4 * (wave - 2) : 0);
-    auto fetch = [&](int t) {
+    auto fetch = [&](int t) { // (the empty statements keep the compiler from merging the kinds of loads into single words with an address each)
         const int t0 = tl.token0(t);
-        if (t0 + K8_TILE <= tl.hi_max) {
-            const int8_t *tile = (wave < 2 ? K : V) + (int64_t)t0 * HD;
-            if (wave < 2) {
+        const bool whole = t0 + K8_TILE <= tl.hi_max; // else: tokens behind the last one any row sees repeat that one
+        if (wave < 2) {
+            const int8_t *p = K + (int64_t)t0 * HD + (whole ? stage_at : min(16 * wave + qi, last_tok - t0) * HD + 16 * grp);
 #pragma unroll
-                for (int p = 0; p < HD / 64; p++) *(uint4 *)&st[4 * p] = *(const uint4 *)(tile + stage_at + 64 * p);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; e++) st[e] = *(const uint32_t *)(tile + stage_at + (e < 4 ? e : 12 + e) * HD);
+            for (int k = 0; k < HD / 64; k++) {
+                const uint4 w = *(const uint4 *)(p + 64 * k);
+                st[4 * k] = w.x, st[4 * k + 1] = w.y, st[4 * k + 2] = w.z, st[4 * k + 3] = w.w;
             }
-        } else if (wave < 2) { // tokens behind the last one any row sees repeat that one
+            asm volatile("; keys" ::: "memory");
+        } else if (whole) {
+            const int8_t *p = V + (int64_t)t0 * HD + stage_at;
 #pragma unroll
-            for (int p = 0; p < HD / 64; p++)
-                *(uint4 *)&st[4 * p] = *(const uint4 *)(K + (int64_t)min(t0 + 16 * wave + qi, last_tok) * HD + 64 * p + 16 * grp);
+            for (int e = 0; e < 8; e++) st[e] = *(const uint32_t *)(p + (e < 4 ? e : 12 + e) * HD);
+            asm volatile("; values" ::: "memory");
         } else {
+            const int8_t *p = V + (int64_t)t0 * HD + VB * qi + (HD == 128 ? 4 * (wave - 2) : 0);
 #pragma unroll
-            for (int e = 0; e < 8; e++)
-                st[e] = *(const uint32_t *)(V + (int64_t)min(t0 + 16 * (e / 4) + 4 * grp + e % 4, last_tok) * HD + VB * qi + (HD == 128 ? 4 * (wave - 2) : 0));
+            for (int e = 0; e < 8; e++) st[e] = *(const uint32_t *)(p + min(16 * (e / 4) + 4 * grp + e % 4, last_tok - t0) * HD);
+            asm volatile("; last values" ::: "memory");
         }
-        if ((wave & 1) == 0 && lane < K8_TILE) {
-            const int tok = t0 + lane;
+        if ((wave & 1) == 0) {
+            const int tok = t0 + (lane & 31);
             ss = (wave ? VS : KS)[min(tok, last_tok)];
             if (wave && !any_sees(tok)) ss = 0.f;
         }
@@ -893,6 +895,7 @@ __global__ __launch_bounds__(256, 3) void kv8_attn_tile_kernel(Kv8View c, Kv8Row
                 *(f16x8 *)&b.frag[wave * NS + 2 * p][lane] = codes_to_half(st[4 * p], st[4 * p + 1]);
                 *(f16x8 *)&b.frag[wave * NS + 2 * p + 1][lane] = codes_to_half(st[4 * p + 2], st[4 * p + 3]);
             }
+            asm volatile("; keys" ::: "memory");
         } else {
             Half8 f[4];
 #pragma unroll
@@ -904,8 +907,9 @@ __global__ __launch_bounds__(256, 3) void kv8_attn_tile_kernel(Kv8View c, Kv8Row
             uint4(*v)[64] = b.frag + 2 * NS + (HD == 128 ? 4 * (wave - 2) : 0);
             if (HD == 128 || wave == 2) *(f16x8 *)&v[0][lane] = f[0].v, *(f16x8 *)&v[1][lane] = f[1].v;
             if (HD == 128 || wave == 3) *(f16x8 *)&v[2][lane] = f[2].v, *(f16x8 *)&v[3][lane] = f[3].v;
+            asm volatile("; values" ::: "memory");
         }
-        if ((wave & 1) == 0 && lane < K8_TILE) (wave ? b.vs : b.ks)[lane] = ss * (wave ? inv_E : qf);
+        if ((wave & 1) == 0) (wave ? b.vs : b.ks)[lane & 31] = ss * (wave ? inv_E : qf); // (two lanes write the same)
     };
     auto consume = [&](int t, const Buf &b, auto masked) {
         constexpr bool MASKED = decltype(masked)::value;
