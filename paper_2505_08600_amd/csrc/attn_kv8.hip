@@ -75,12 +75,17 @@ __global__ __launch_bounds__(256) void kv8_attn_generic_kernel(Kv8View c, Kv8Row
     const Kv8Seen seen = kv8_seen(a, s.len, i, kv8_capacity(c, s.b));
     const int n = seen.n_first + (seen.hi - seen.lo);
     const int64_t base = (int64_t)(h / (a.n_heads / c.kv_heads)) * c.tokens + c.off[s.b];
-    for (int d = tid; d < hd; d += 256)
+    bool bad = false;
+    for (int d = tid; d < hd; d += 256) {
         sq[d] = a.dtype == SD_BF16 ? to_float(((const bf16_t *)a.q)[r * a.q_row + h * a.q_head + d]) : ((const float *)a.q)[r * a.q_row + h * a.q_head + d];
+        bad |= !(fabsf(sq[d]) < INFINITY);
+    }
+    const float scale = __syncthreads_or(bad) ? NAN : a.scale; // (everything of such a row is NaN)
     // (a thread of the second step owns four dimensions, dg, of the tokens tg, tg + n_tg, ...)
     const int n_dg = hd / 4, dg = tid % n_dg, tg = tid / n_dg, n_tg = 256 / n_dg;
     float m = -INFINITY, l = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
     for (int u0 = 0; u0 < n; u0 += KG_CHUNK) {
+#pragma clang fp contract(off) // x - m_ref is a difference of rounded scores: 0 for the largest, however large they are
         __syncthreads(); // sq is there; nobody reads sp and red any more
         const int u = u0 + tid;
         const int t = u < seen.n_first ? u : seen.lo + (u - seen.n_first);
@@ -94,7 +99,7 @@ __global__ __launch_bounds__(256) void kv8_attn_generic_kernel(Kv8View c, Kv8Row
 #pragma unroll
                 for (int e = 0; e < 16; e++) dot = fmaf(sq[d + e], (float)((int32_t)(ww[e / 4] << (24 - 8 * (e % 4))) >> 24), dot);
             }
-            x = dot * c.ks[base + t] * a.scale;
+            x = dot * c.ks[base + t] * scale;
             vs = c.vs[base + t];
         }
         float mx = x;
@@ -192,6 +197,13 @@ __device__ __forceinline__ float rows4_max(float v)
     const auto b = __builtin_amdgcn_permlane32_swap(u, u, false, false);
     return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
+__device__ __forceinline__ uint32_t rows4_most(uint32_t u)
+{
+    const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    u = max(a[0], a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return max(b[0], b[1]);
+}
 __device__ __forceinline__ float rows4_sum(float v)
 {
     unsigned u = __float_as_uint(v);
@@ -206,7 +218,7 @@ __device__ __forceinline__ float rows4_sum(float v)
 // w0 on; T in all.  hi_max / lo_min: of any row, hi_min / lo_max: of every row.
 struct Kv8Tiles {
     int hi_max, hi_min, lo_min, lo_max, n_sink, w0, T;
-    __device__ __forceinline__ int token0(int t) const { return (t < n_sink ? t : w0 + (t - n_sink)) * K8_TILE; }
+    __device__ __forceinline__ int token0(int t) const { return (t + (t < n_sink ? 0 : w0 - n_sink)) * K8_TILE; }
 };
 __device__ __forceinline__ Kv8Tiles kv8_tiles(const Kv8Attn &a, int len, int i0, int i1, int cap)
 {
@@ -222,7 +234,11 @@ __device__ __forceinline__ Kv8Tiles kv8_tiles(const Kv8Attn &a, int len, int i0,
 // does not matter to the sums), so that the loops over either kind have one body each.
 struct Kv8Order {
     int t_begin, f0, f1, n_left, n_edge, n;
-    __device__ __forceinline__ int tile(int u) const { return u < n_left ? t_begin + u : u < n_edge ? f1 + (u - n_left) : f0 + (u - n_edge); }
+    __device__ __forceinline__ int tile(int u) const
+    {
+        const int far = u < n_edge ? f1 - n_left : f0 - n_edge;
+        return u + (u < n_left ? t_begin : far);
+    }
 };
 __device__ __forceinline__ Kv8Order kv8_order(const Kv8Tiles &tl, int t_begin, int t_end)
 {
@@ -238,49 +254,45 @@ __device__ __forceinline__ Kv8Order kv8_order(const Kv8Tiles &tl, int t_begin, i
 // longer than the launch was told of, an even share.
 __device__ __forceinline__ int kv8_per_split(int T, int S, int per) { return max(per, (T + S - 1) / S); }
 
-// 16 adjacent elements of a query row
+// 16 adjacent elements of a query row, as they lie
 template <int TERMS>
-__device__ __forceinline__ void load_q16(const Kv8Attn &a, bool wide, int64_t at, float *x)
-{
-    if constexpr (TERMS == 1) {
-        const bf16_t *p = (const bf16_t *)a.q + at;
-        if (wide) {
-#pragma unroll
-            for (int v = 0; v < 2; v++) {
-                const uint4 w = ((const uint4 *)p)[v];
-                const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-                for (int e = 0; e < 4; e++) x[8 * v + 2 * e] = __uint_as_float(u[e] << 16), x[8 * v + 2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 16; e++) x[e] = to_float(p[e]);
-        }
-    } else {
-        const float *p = (const float *)a.q + at;
-        if (wide) {
-#pragma unroll
-            for (int v = 0; v < 4; v++) {
-                const float4 w = ((const float4 *)p)[v];
-                x[4 * v] = w.x, x[4 * v + 1] = w.y, x[4 * v + 2] = w.z, x[4 * v + 3] = w.w;
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 16; e++) x[e] = p[e];
-        }
+struct Q16 {
+    static constexpr int N = 8 * TERMS;
+    uint32_t w[N];
+    __device__ __forceinline__ float operator[](int e) const
+    {
+        if constexpr (TERMS == 1) return __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+        else return __uint_as_float(w[e]);
     }
-}
-// Queries are scaled by one power of two for all rows that share it, so that the largest element (mx) lies in [2^bits, 2^(bits + 1)).
-struct QScale {
-    float up, down; // there, and back
 };
-__device__ __forceinline__ QScale q_scale(float mx, int bits)
+template <int TERMS>
+__device__ __forceinline__ Q16<TERMS> load_q16(const Kv8Attn &a, bool wide, int64_t at)
 {
-    const int e = min(127, max(-100, (int)(__float_as_uint(mx) >> 23) - 127)); // (kept where both factors are normal numbers)
-    return QScale{__uint_as_float((uint32_t)(127 + bits - e) << 23), __uint_as_float((uint32_t)(127 - bits + e) << 23)};
+    Q16<TERMS> r;
+    if (wide) {
+        const uint4 *p = (const uint4 *)((const char *)a.q + at * (TERMS == 1 ? 2 : 4));
+#pragma unroll
+        for (int v = 0; v < r.N / 4; v++) {
+            const uint4 w = p[v];
+            r.w[4 * v] = w.x, r.w[4 * v + 1] = w.y, r.w[4 * v + 2] = w.z, r.w[4 * v + 3] = w.w;
+        }
+    } else if constexpr (TERMS == 1) {
+        const uint16_t *p = (const uint16_t *)a.q + at;
+#pragma unroll
+        for (int e = 0; e < 8; e++) r.w[e] = p[2 * e] | (uint32_t)p[2 * e + 1] << 16;
+    } else {
+        const uint32_t *p = (const uint32_t *)a.q + at;
+#pragma unroll
+        for (int e = 0; e < 16; e++) r.w[e] = p[e];
+    }
+    return r;
 }
+// Queries are scaled by a power of two, so that a largest element (of magnitude bits mx) lies in [2^bits, 2^(bits + 1)): 2^(bits - q_exp(mx)).
+#define K8_INF 0x7f800000u // bits of a magnitude from here on: infinite, or not a number
+__device__ __forceinline__ int q_exp(uint32_t mx) { return min(127, max(-100, (int)(mx >> 23) - 127)); } // (kept where 2^+-(e - bits) are normal numbers)
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
 // As halves (bits = 14): one holds every bf16 element down to 2^-31 of the largest exactly, two hold 22 bits of an fp32 one, and what
-// smaller elements lose is 2^-39 of the largest - nothing in a score.
+// smaller elements lose is 2^-39 of the largest.
 // The Q^T operands of a 16-row set: lane (qi, grp) takes dimensions 64 j + 16 grp + 8 s .. + 8 into step 2 j + s, the order a 16-byte
 // piece of the codes has them in.
 template <int HD, int TERMS>
@@ -300,27 +312,35 @@ __device__ __forceinline__ void query_operands(const float (&x)[HD / 4], float u
     }
 }
 // MT sets of 16 rows from product row m0 on (row i, head g of the group: m = i * grps + g), HD / 4 elements a lane: of dimensions
-// 64 j + 16 grp .. + 16 for each j.  Returns the largest magnitude.
+// 64 j + 16 grp .. + 16 for each j.
 template <int HD, int MT, int TERMS>
-__device__ __forceinline__ float load_rows(const Kv8Attn &a, const Kv8Seq &sq, int n_rows, int kvh, int grps, int m0, float (&x)[MT][HD / 4])
+__device__ __forceinline__ void load_rows(const Kv8Attn &a, const Kv8Seq &sq, int n_rows, int kvh, int grps, int m0, Q16<TERMS> (&raw)[MT][HD / 64])
 {
     const int qi = threadIdx.x & 15, grp = (threadIdx.x & 63) >> 4;
     const bool wide = kv8_wide(a.q, a.q_row, a.q_head, a.dtype);
-    float mx = 0.f;
 #pragma unroll
     for (int mt = 0; mt < MT; mt++) {
         const int m = m0 + 16 * mt + qi, i = (unsigned)m / (unsigned)grps, g = m - i * grps;
 #pragma unroll
-        for (int e = 0; e < HD / 4; e++) x[mt][e] = 0.f;
-        if (i < n_rows) {
+        for (int j = 0; j < HD / 64; j++) raw[mt][j] = {};
+        if ((unsigned)i < (unsigned)n_rows) {
             const int64_t at = (int64_t)(sq.row0 + i) * a.q_row + (int64_t)(kvh * grps + g) * a.q_head;
 #pragma unroll
-            for (int j = 0; j < HD / 64; j++) load_q16<TERMS>(a, wide, at + 64 * j + 16 * grp, &x[mt][16 * j]);
+            for (int j = 0; j < HD / 64; j++) raw[mt][j] = load_q16<TERMS>(a, wide, at + 64 * j + 16 * grp);
         }
-#pragma unroll
-        for (int e = 0; e < HD / 4; e++) mx = fmaxf(mx, fabsf(x[mt][e]));
     }
-    return mx;
+}
+// ... as numbers, and the bits of the largest magnitude of the lane's row (a NaN's are above infinity's, which are above every number's)
+template <int HD, int TERMS>
+__device__ __forceinline__ uint32_t row_values(const Q16<TERMS> (&raw)[HD / 64], float (&x)[HD / 4])
+{
+    uint32_t mx = 0;
+#pragma unroll
+    for (int e = 0; e < HD / 4; e++) {
+        x[e] = raw[e / 16][e % 16];
+        mx = max(mx, __float_as_uint(x[e]) & 0x7fffffffu);
+    }
+    return rows4_most(mx);
 }
 // over the wave
 __device__ __forceinline__ float wave_max(float v)
@@ -330,9 +350,11 @@ __device__ __forceinline__ float wave_max(float v)
 }
 
 // How the tiles of all (sequence, cache head, set of rows) units are dealt out.  Units stand in a row, a sequence's next to each other and as
-// long as what any row of the sequence sees (and K8_UNIT_COST more: 32 x 6 rows over up to 4096 tokens 146 us without, 140 with); block b takes the stretch [b * chunk, (b + 1) * chunk), which may reach over several units
-// and cover parts of the first and the last: every block has the same work, whatever the lengths.  With too little work for that
-// (`cross` = false) units are rounded up to whole stretches instead, and no block has parts of two.
+// long as what any row of the sequence sees and K8_UNIT_COST more (32 x 6 rows over up to 4096 tokens 146 us without, 140 with); block b
+// takes the stretch [b * chunk, (b + 1) * chunk), which may reach over several units and cover parts of the first and the last: every
+// block has the same work, whatever the lengths.  With too little work for that (`cross` = false) units are rounded up to whole
+// stretches instead, and no block has parts of two.
+// Positions in the row are 32-bit: they count 2^grain tiles each, grain > 0 only where units or tiles are very many.
 // Tiles of a unit of sequence j and number of its units (each lane for a j of its own); {0, 0}: nothing to do.
 struct Kv8Units {
     int T, n;
@@ -342,7 +364,7 @@ __device__ __forceinline__ Kv8Units kv8_units(const Kv8View &c, const Kv8Rows &r
 {
     if (j >= rw.n) return Kv8Units{0, 0};
     const int b = rw.seq_ids ? rw.seq_ids[j * rw.group] : j;
-    const int n_rows = rw.row_start ? rw.row_start[j + 1] - rw.row_start[j] : rw.rows; // (unused slots of the path count: they are written too)
+    const int n_rows = kv8_last_row(rw, j) - kv8_first_row(rw, j); // (unused slots of the path count: they are written too)
     if (b < 0 || b >= c.n_seq || n_rows < 1) return Kv8Units{0, 0};
     const int T = kv8_tiles(a, kv8_length(rw.len[rw.path ? j * rw.group : b]), 0, n_rows - 1, kv8_capacity(c, b)).T;
     return Kv8Units{max(T, 1), (n_rows * (a.n_heads / c.kv_heads) + SET - 1) / SET * c.kv_heads}; // (rows that see nothing are written: a tile at least)
@@ -367,13 +389,18 @@ __device__ __forceinline__ int wave_upto(int v) // sum of the lanes up to this o
     const int a = __builtin_amdgcn_readlane(v, 15), b = __builtin_amdgcn_readlane(v, 31), c = __builtin_amdgcn_readlane(v, 47), row = (threadIdx.x & 63) >> 4;
     return v + (row > 0 ? a : 0) + (row > 1 ? b : 0) + (row > 2 ? c : 0);
 }
-// The deal, and the first 64 sequences' share of it in the lanes.  2^31 tiles would be 8 TiB of codes.
+// The deal, and the first 64 sequences' share of it in the lanes.
 struct Kv8Deal {
-    int total, chunk; // tiles in the row, and of a stretch
+    int total, chunk; // positions in the row, and of a stretch
+    int grain;
     bool cross;
     Kv8Units mine;    // of sequence `lane`
     int upto;         // where its units end
-    __device__ __forceinline__ int length(int T) const { return cross ? T + K8_UNIT_COST : (int)(((unsigned)T + chunk - 1) / (unsigned)chunk) * chunk; }
+    __device__ __forceinline__ int length(int T) const
+    {
+        const int t = grain ? (T + (1 << grain) - 1) >> grain : T;
+        return cross ? t + K8_UNIT_COST : (int)(((unsigned)t + chunk - 1) / (unsigned)chunk) * chunk;
+    }
 };
 // S: parts a unit may end up in; goal: blocks that are wanted.  Uniform over the grid.
 template <int SET>
@@ -382,27 +409,26 @@ __device__ __forceinline__ Kv8Deal kv8_deal(const Kv8View &c, const Kv8Rows &rw,
     const int lane = threadIdx.x & 63;
     Kv8Deal d;
     d.mine = kv8_units<SET>(c, rw, a, lane);
-    int W = (d.mine.T + K8_UNIT_COST) * d.mine.n, T_max = max(1, d.mine.T);
-    for (int j = lane + 64; j - lane < rw.n; j += 64) {
-        const Kv8Units u = kv8_units<SET>(c, rw, a, j);
-        W += (u.T + K8_UNIT_COST) * u.n, T_max = max(T_max, u.T);
-    }
-    W = wave_total(W), T_max = wave_most(T_max);
+    auto over_all = [&](auto f) { // sum of f(units of a sequence) over all
+        int v = f(d.mine);
+        for (int j = lane + 64; j - lane < rw.n; j += 64) v += f(kv8_units<SET>(c, rw, a, j));
+        return wave_total(v);
+    };
+    int T_max = max(1, d.mine.T);
+    for (int j = lane + 64; j - lane < rw.n; j += 64) T_max = max(T_max, kv8_units<SET>(c, rw, a, j).T);
+    T_max = wave_most(T_max);
+    // at most `units` of them (2^24: kv8_plan), so that 2^29 positions hold all and the longest is no longer than 2^18
+    const uint64_t units = (uint64_t)(unsigned)a.total_rows * (unsigned)c.kv_heads, most = units * (unsigned)(T_max + K8_UNIT_COST) >> 29 | (unsigned)T_max >> 18;
+    d.grain = most ? 64 - __builtin_clzll(most) : 0;
+    T_max = (T_max + (1 << d.grain) - 1) >> d.grain;
+    d.cross = true;
+    const int W = over_all([&](Kv8Units u) { return d.length(u.T) * u.n; });
     d.cross = S > 1 && W > goal * K8_MIN_TILES;
     // (a stretch that starts inside a unit makes one more part of it)
     d.chunk = d.cross ? (int)max((unsigned)(W + goal - 1) / (unsigned)goal, (unsigned)(T_max + K8_UNIT_COST + S - 2) / (unsigned)(S - 1))
               : S > 1 ? max(K8_MIN_TILES, (int)((unsigned)(T_max + S - 1) / (unsigned)S)) : T_max;
-    const int len = d.length(d.mine.T) * d.mine.n;
-    d.upto = wave_upto(len);
-    d.total = W;
-    if (!d.cross) {
-        W = len;
-        for (int j = lane + 64; j - lane < rw.n; j += 64) {
-            const Kv8Units u = kv8_units<SET>(c, rw, a, j);
-            W += d.length(u.T) * u.n;
-        }
-        d.total = wave_total(W);
-    }
+    d.upto = wave_upto(d.length(d.mine.T) * d.mine.n);
+    d.total = d.cross ? W : over_all([&](Kv8Units u) { return d.length(u.T) * u.n; });
     return d;
 }
 // The sequence that position `at` < total lies in, its unit's length, where its units start and end.
@@ -419,7 +445,7 @@ __device__ __forceinline__ Kv8Found kv8_find(const Kv8View &c, const Kv8Rows &rw
         if (behind || j0 + 64 >= rw.n) {
             const int l = __builtin_amdgcn_readfirstlane(behind ? __ffsll((unsigned long long)behind) - 1 : 63);
             const int len = d.length(__builtin_amdgcn_readlane(u.T, l)), end = __builtin_amdgcn_readlane(upto, l);
-            return Kv8Found{j0 + l, len, end - len * __builtin_amdgcn_readlane(u.n, l), end};
+            return Kv8Found{min(j0 + l, rw.n - 1), len, end - len * __builtin_amdgcn_readlane(u.n, l), end};
         }
         before = __builtin_amdgcn_readlane(upto, 63);
         u = kv8_units<SET>(c, rw, a, j0 + 64 + (threadIdx.x & 63));
@@ -507,11 +533,12 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void kv8_attn_stream_kernel(K
         if (at >= f.end || at < f.start) f = kv8_find<SET>(c, rw, a, deal, at);
         const int j = f.j, unit = (unsigned)(at - f.start) / (unsigned)f.len;
         const int u0 = f.start + unit * f.len; // the unit's first position
-        const int t_begin = at - u0, first_blk = (unsigned)u0 / (unsigned)deal.chunk, split = blk - first_blk;
+        const int t_begin = (at - u0) << deal.grain, first_blk = (unsigned)u0 / (unsigned)deal.chunk, split = blk - first_blk;
         const bool only = u0 + f.len <= (first_blk + 1) * deal.chunk; // the whole unit is this block's
         const int set = (unsigned)unit / (unsigned)c.kv_heads, kvh = unit - set * c.kv_heads, m0 = set * SET;
-        const int n_here = min(end, u0 + f.len) - at;
+        const int n_here = max(1, min(end, u0 + f.len) - at); // (always one: should rows overlap, which row_start must not say, the loop still ends)
         at += n_here;
+        const int t_stop = (int)min((int64_t)1 << 30, (int64_t)t_begin + ((int64_t)n_here << deal.grain));
         const Kv8Seq sq = kv8_seq(c, rw, j);
         const int n_rows = sq.n_rows, all = (rw.path ? rw.rows : n_rows) * grps; // (unused slots of the path receive zeros)
         const int cap = kv8_capacity(c, sq.b);
@@ -522,12 +549,12 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void kv8_attn_stream_kernel(K
         const int i_first = (unsigned)m0 / (unsigned)grps, i_last = min(n_rows - 1, (int)((unsigned)(m0 + SET - 1) / (unsigned)grps));
         Kv8Tiles tl = {};
         if (i_first < n_rows) {
-            tl = kv8_tiles(a, sq.len, 0, (rw.row_start ? n_rows : rw.rows) - 1, cap);
+            tl = kv8_tiles(a, sq.len, 0, (rw.path ? rw.rows : n_rows) - 1, cap);
             const Kv8Seen first = kv8_seen(a, sq.len, i_first, cap), last = kv8_seen(a, sq.len, i_last, cap);
             tl.hi_min = first.hi, tl.lo_max = last.lo;
             tl.hi_max = last.hi;
         }
-        const int t_end = min(min(tl.T, tl.n_sink + (tl.hi_max + K8_TILE - 1) / K8_TILE - tl.w0), t_begin + n_here);
+        const int t_end = min(min(tl.T, tl.n_sink + (tl.hi_max + K8_TILE - 1) / K8_TILE - tl.w0), t_stop);
         float m_run[MT], l_run[MT];
         Kv8Seen seen[MT]; // of the lane's row in each set
         f32x4 o[MT][ND];
@@ -546,14 +573,18 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void kv8_attn_stream_kernel(K
         // One tile's bytes: they are asked for where the tile before it has used the registers up, K and the scales behind the score
         // products, V behind the output products.
         K8Regs<HD> r;
-        auto load_k = [&](int t) {
+        // (edge: a tile that may reach behind the last token.  Those between the edges are loaded without the question, from a uniform base:
+        // 4 x 65536 tokens of 8 heads of 128 for 6 x 32 query rows 85 us with the question everywhere, 79 so.)
+        auto load_k = [&](int t, auto edge) {
             const int t0 = tl.token0(t);
-            if (t0 + K8_TILE <= tl.hi_max) { // (uniform) a whole tile: one address and constant offsets
+            if (!decltype(edge)::value || t0 + K8_TILE <= tl.hi_max) { // (uniform) a whole tile: one address and constant offsets
                 const int8_t *kt = K + (int64_t)t0 * HD;
+                uint32_t lane_at = k_lane;
+                asm volatile("" : "+v"(lane_at)); // (kept 32 bits wide next to the loads, whose base is uniform)
 #pragma unroll
                 for (int h = 0; h < 2; h++)
 #pragma unroll
-                    for (int p = 0; p < HD / 64; p++) r.k[h][p] = read_once<uint4>(kt + k_lane + (16 * h * HD + 64 * p));
+                    for (int p = 0; p < HD / 64; p++) r.k[h][p] = read_once<uint4>(kt + lane_at + (16 * h * HD + 64 * p));
             } else { // tokens behind the last one any row sees repeat that one
 #pragma unroll
                 for (int h = 0; h < 2; h++)
@@ -563,12 +594,14 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void kv8_attn_stream_kernel(K
             const int tok = t0 + (lane & 31);
             r.sc = (lane < 32 ? KS : VS)[min(tok, last_tok)];
         };
-        auto load_v = [&](int t) {
+        auto load_v = [&](int t, auto edge) {
             const int t0 = tl.token0(t);
-            if (t0 + K8_TILE <= tl.hi_max) {
+            if (!decltype(edge)::value || t0 + K8_TILE <= tl.hi_max) {
                 const int8_t *vt = V + (int64_t)t0 * HD;
+                uint32_t lane_at = v_lane;
+                asm volatile("" : "+v"(lane_at));
 #pragma unroll
-                for (int e = 0; e < 8; e++) r.v[e] = read_once<typename K8Regs<HD>::VRow>(vt + v_lane + (e < 4 ? e : 12 + e) * HD);
+                for (int e = 0; e < 8; e++) r.v[e] = read_once<typename K8Regs<HD>::VRow>(vt + lane_at + (e < 4 ? e : 12 + e) * HD);
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; e++)
@@ -576,18 +609,24 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void kv8_attn_stream_kernel(K
             }
         };
         const Kv8Order od = kv8_order(tl, t_begin, t_end);
-        if (wave < od.n) { // the first tile is on its way while the queries are read
-            load_k(od.tile(wave));
-            load_v(od.tile(wave));
+        Q16<TERMS> raw[MT][HD / 64];
+        load_rows<HD, MT, TERMS>(a, sq, n_rows, kvh, grps, m0, raw);
+        if (wave < od.n) { // the first tile is on its way while the queries are looked at
+            load_k(od.tile(wave), std::true_type{});
+            load_v(od.tile(wave), std::true_type{});
         }
+        // Each row has a scale of its own, whatever the rows beside it hold: a score is its product times the token's scale, a.scale / 2^21
+        // (both in sS) and 2^e (q2e, folded into the exponential's argument).  Of a row with a NaN or an infinity everything is NaN.
         i32x4 q[MT][3][HD / 64];
-        float qf; // what a product has to be multiplied by to be a score
-        {
-            float x[MT][HD / 4];
-            const QScale qs = q_scale(wave_max_dpp(load_rows<HD, MT, TERMS>(a, sq, n_rows, kvh, grps, m0, x)), 21); // (the same in every wave: they hold the same rows)
-            qf = qs.down * a.scale;
+        float q2e[MT];
+        const float qf = a.scale * pow2(-21);
 #pragma unroll
-            for (int mt = 0; mt < MT; mt++) query_digits<HD>(x[mt], qs.up, q[mt]);
+        for (int mt = 0; mt < MT; mt++) {
+            float x[HD / 4];
+            const uint32_t mx = row_values<HD, TERMS>(raw[mt], x);
+            const int e = q_exp(mx);
+            query_digits<HD>(x, pow2(21 - e), q[mt]);
+            q2e[mt] = mx >= K8_INF && (seen[mt].hi > seen[mt].lo || seen[mt].n_first) ? NAN : pow2(e);
         }
         // (t_next is asked for whether it is wanted or not: with loads that may be left out, the wait for K would have to be one for V too)
         auto consume = [&](int t, int t_next, auto masked) {
@@ -626,7 +665,7 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void kv8_attn_stream_kernel(K
             const f32x4 va = *(const f32x4 *)&sS[wave][32 + 4 * grp], vb = *(const f32x4 *)&sS[wave][48 + 4 * grp];
             asm volatile("" ::: "memory");
             __builtin_amdgcn_sched_barrier(0);
-            load_k(t_next);
+            load_k(t_next, masked);
             __builtin_amdgcn_sched_barrier(0);
             Half8 ph[MT][TERMS];
 #pragma unroll
@@ -644,7 +683,7 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void kv8_attn_stream_kernel(K
                     }
                     mx = fmaxf(mx, x[e]);
                 }
-                const float m_new = fmaxf(m_run[mt], rows4_max(mx));
+                const float m_new = fmaxf(m_run[mt], rows4_max(mx) * q2e[mt]);
                 const float ref = m_new == -INFINITY ? 0.f : m_new;
                 const float corr = __builtin_amdgcn_exp2f(m_run[mt] - ref), corr_o = corr * shrink;
                 m_run[mt] = m_new;
@@ -654,7 +693,7 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void kv8_attn_stream_kernel(K
                     float p[2];
 #pragma unroll
                     for (int f = 0; f < 2; f++) {
-                        p[f] = __builtin_amdgcn_exp2f(x[e + f] - ref);
+                        p[f] = __builtin_amdgcn_exp2f(fmaf(x[e + f], q2e[mt], -ref));
                         sum += p[f];
                         p[f] *= e < 4 ? va[e + f] : vb[e - 4 + f];
                         if (MASKED) p[f] = vis[e + f] ? p[f] : 0.f;
@@ -692,7 +731,7 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void kv8_attn_stream_kernel(K
                             o[mt][4 * w + b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[b].v, ph[mt][u].v, o[mt][4 * w + b], 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            load_v(t_next);
+            load_v(t_next, masked);
             __builtin_amdgcn_sched_barrier(0);
         };
         if (wave < od.n) {
@@ -717,7 +756,7 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void kv8_attn_stream_kernel(K
                         f32x4{o[mt][b][r], o[mt][b + 1][r], o[mt][b + 2][r], o[mt][b + 3][r]} * back;
             __syncthreads();
             const int m = m0 + 16 * mt + row;
-            if (m >= all) continue;
+            if ((unsigned)m >= (unsigned)all) continue;
             const float M = fmaxf(fmaxf(sM[0][row], sM[1][row]), fmaxf(sM[2][row], sM[3][row])), ref = M == -INFINITY ? 0.f : M;
             float v[VB], L = 0.f;
 #pragma unroll
@@ -741,7 +780,7 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void kv8_attn_stream_kernel(K
                 for (int d = 0; d < VB; d++) v[d] = i >= n_rows ? 0.f : v[d] * g;
                 kv8_store_run<VB>(a, kv8_wide(a.out, a.o_row, a.o_head, a.dtype), r, h, HD, d0, v);
                 if (a.lse && d0 == 0) a.lse[(int64_t)r * a.n_heads + h] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
-            } else {
+            } else if ((unsigned)split < (unsigned)S) { // (always, but for such rows)
                 float *p = part + (((int64_t)r * a.n_heads + h) * S + split) * (HD + 4);
 #pragma unroll
                 for (int d = 0; d < VB; d += 4) *(float4 *)(p + 4 + d0 + d) = make_float4(v[d], v[d + 1], v[d + 2], v[d + 3]);
@@ -772,7 +811,7 @@ __global__ __launch_bounds__(256, 3) void kv8_attn_tile_kernel(Kv8View c, Kv8Row
         float ks[K8_TILE], vs[K8_TILE];
     };
     __shared__ Buf buf[2];
-    __shared__ float red[4];
+    __shared__ float red[4], row_factor[4][MT * 16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int qi = lane & 15, grp = lane >> 4;
     const int kvh = blockIdx.x % c.kv_heads, split = blockIdx.y, grps = a.n_heads / c.kv_heads;
@@ -787,7 +826,7 @@ __global__ __launch_bounds__(256, 3) void kv8_attn_tile_kernel(Kv8View c, Kv8Row
             int found = -1, left = b;
             for (int j0 = 0; j0 < rw.n && found < 0; j0 += 64) {
                 const int jj = j0 + lane;
-                const int n = jj < rw.n ? rw.row_start[jj + 1] - rw.row_start[jj] : 0;
+                const int n = jj < rw.n ? kv8_last_row(rw, jj) - kv8_first_row(rw, jj) : 0;
                 const int upto = wave_upto(n > 0 ? (n * grps + ROWS - 1) / ROWS : 0);
                 const uint64_t behind = __ballot(upto > left);
                 if (behind) {
@@ -825,15 +864,6 @@ __global__ __launch_bounds__(256, 3) void kv8_attn_tile_kernel(Kv8View c, Kv8Row
         __syncthreads();
         return fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
     };
-    f16x8 q[MT][TERMS][NS];
-    float qf; // what a product has to be multiplied by to be a score
-    {
-        float x[MT][HD / 4];
-        const QScale qs = q_scale(block_max(load_rows<HD, MT, TERMS>(a, sq, n_rows, kvh, grps, m0, x)), 14);
-        qf = qs.down * a.scale;
-#pragma unroll
-        for (int mt = 0; mt < MT; mt++) query_operands<HD, TERMS>(x[mt], qs.up, q[mt]);
-    }
     float m_run[MT], l_run[MT];
     Kv8Seen seen[MT];
     f32x4 o[MT][ND];
@@ -845,6 +875,36 @@ __global__ __launch_bounds__(256, 3) void kv8_attn_tile_kernel(Kv8View c, Kv8Row
         m_run[mt] = -INFINITY, l_run[mt] = 0.f;
 #pragma unroll
         for (int d = 0; d < ND; d++) o[mt][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    // One scale for the rows of the block, from the largest number among them: what a row's elements lose is 2^-39 of that, less than 2^-22 of
+    // the row's own largest, unless that is 2^17 times smaller.  Such a row has a scale of its own, and so has one with a NaN or an
+    // infinity, whose scores are all NaN; only then are products looked up a factor (`uneven`): a multiplication of every score makes 351 us
+    // of a prompt 370.
+    f16x8 q[MT][TERMS][NS];
+    float qf; // what a product has to be multiplied by to be a score
+    bool uneven;
+    {
+        Q16<TERMS> raw[MT][HD / 64];
+        float x[MT][HD / 4], most = 0.f;
+        uint32_t mx[MT];
+        load_rows<HD, MT, TERMS>(a, sq, n_rows, kvh, grps, m0, raw);
+#pragma unroll
+        for (int mt = 0; mt < MT; mt++) {
+            mx[mt] = row_values<HD, TERMS>(raw[mt], x[mt]);
+            most = fmaxf(most, mx[mt] < K8_INF ? __uint_as_float(mx[mt]) : 0.f);
+        }
+        const int e = q_exp(__float_as_uint(block_max(most)));
+        qf = a.scale * pow2(e - 14);
+        bool odd = false;
+#pragma unroll
+        for (int mt = 0; mt < MT; mt++) {
+            const int own = q_exp(mx[mt]);
+            const bool small = mx[mt] && own < e - 16, bad = mx[mt] >= K8_INF && (seen[mt].hi > seen[mt].lo || seen[mt].n_first);
+            query_operands<HD, TERMS>(x[mt], pow2(14 - (small ? own : e)), q[mt]);
+            if (grp == 0) row_factor[wave][16 * mt + qi] = bad ? NAN : small ? ldexpf(1.f, own - e) : 1.f;
+            odd |= small || bad;
+        }
+        uneven = __syncthreads_or(odd);
     }
     auto any_sees = [&](int tok) { return tok < tl.hi_max && (tok >= tl.lo_min || tok < a.sinks); };
     float big = 0.f;
@@ -860,21 +920,25 @@ __global__ __launch_bounds__(256, 3) void kv8_attn_tile_kernel(Kv8View c, Kv8Row
     float ss = 0.f;
     // (byte offsets inside a tile)
     const uint32_t stage_at = wave < 2 ? (16 * wave + qi) * HD + 16 * grp : 4 * grp * HD + VB * qi + (HD == 128 ? 4 * (wave - 2) : 0);
-    auto fetch = [&](int t) { // (the empty statements keep the compiler from merging the kinds of loads into single words with an address each)
+    auto fetch = [&](int t, auto edge) { // (the empty statements keep the compiler from merging the kinds of loads into single words with an address each)
         const int t0 = tl.token0(t);
-        const bool whole = t0 + K8_TILE <= tl.hi_max; // else: tokens behind the last one any row sees repeat that one
+        const bool whole = !decltype(edge)::value || t0 + K8_TILE <= tl.hi_max; // else: tokens behind the last one any row sees repeat that one
         if (wave < 2) {
-            const int8_t *p = K + (int64_t)t0 * HD + (whole ? stage_at : min(16 * wave + qi, last_tok - t0) * HD + 16 * grp);
+            const int8_t *p = K + (int64_t)t0 * HD;
+            uint32_t at = whole ? stage_at : min(16 * wave + qi, last_tok - t0) * HD + 16 * grp;
+            asm volatile("" : "+v"(at)); // (kept 32 bits wide next to the loads, whose base is uniform)
 #pragma unroll
             for (int k = 0; k < HD / 64; k++) {
-                const uint4 w = *(const uint4 *)(p + 64 * k);
+                const uint4 w = *(const uint4 *)(p + at + 64 * k);
                 st[4 * k] = w.x, st[4 * k + 1] = w.y, st[4 * k + 2] = w.z, st[4 * k + 3] = w.w;
             }
             asm volatile("; keys" ::: "memory");
         } else if (whole) {
-            const int8_t *p = V + (int64_t)t0 * HD + stage_at;
+            const int8_t *p = V + (int64_t)t0 * HD;
+            uint32_t at = stage_at;
+            asm volatile("" : "+v"(at));
 #pragma unroll
-            for (int e = 0; e < 8; e++) st[e] = *(const uint32_t *)(p + (e < 4 ? e : 12 + e) * HD);
+            for (int e = 0; e < 8; e++) st[e] = *(const uint32_t *)(p + at + (e < 4 ? e : 12 + e) * HD);
             asm volatile("; values" ::: "memory");
         } else {
             const int8_t *p = V + (int64_t)t0 * HD + VB * qi + (HD == 128 ? 4 * (wave - 2) : 0);
@@ -927,6 +991,14 @@ __global__ __launch_bounds__(256, 3) void kv8_attn_tile_kernel(Kv8View c, Kv8Row
 #pragma unroll
                     for (int w = 0; w < TERMS; w++) s[mt][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[mt][w][p], s[mt][h], 0, 0, 0);
             }
+        if (uneven) {
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (int mt = 0; mt < MT; mt++) {
+                const float f = row_factor[wave][16 * mt + qi];
+                s[mt][0] *= f, s[mt][1] *= f;
+            }
+        }
         __builtin_amdgcn_sched_barrier(0);
         f32x4 ks[2], vs[2];
 #pragma unroll
@@ -948,6 +1020,7 @@ __global__ __launch_bounds__(256, 3) void kv8_attn_tile_kernel(Kv8View c, Kv8Row
                 mx = fmaxf(mx, y[e]);
             }
             if (__any(mx > K8_LAZY)) { // (from the start, where m_run is -infinity, too)
+#pragma clang fp contract(off) // the maximum is one of the rounded scores: what they are off by must not be left over from their difference
                 asm volatile("" ::: "memory");
                 mx = -INFINITY;
 #pragma unroll
@@ -996,25 +1069,25 @@ __global__ __launch_bounds__(256, 3) void kv8_attn_tile_kernel(Kv8View c, Kv8Row
     const int n = od.n;
     auto tile_at = [&](int u) { return od.tile(u); };
     if (n > 0) {
-        fetch(tile_at(0));
+        fetch(tile_at(0), std::true_type{});
         stage(buf[0]);
-        if (n > 1) fetch(tile_at(1));
-        auto turn = [&](int u) { // -> this turn's tile, staged
+        if (n > 1) fetch(tile_at(1), std::true_type{});
+        auto turn = [&](int u, auto edge) { // -> this turn's tile, staged
             Buf &now = buf[u & 1], &next = buf[(u + 1) & 1];
             __syncthreads(); // `now` is complete, and nobody reads `next` any more
             if (u + 1 < n) stage(next);
             __builtin_amdgcn_sched_barrier(0);
-            if (u + 2 < n) fetch(tile_at(u + 2));
+            if (u + 2 < n) fetch(tile_at(u + 2), edge);
             __builtin_amdgcn_sched_barrier(0);
             return &now;
         };
         int u = 0;
         for (; u < od.n_edge; u++) {
-            const Buf *b = turn(u);
+            const Buf *b = turn(u, std::true_type{});
             const int t = tile_at(u), t0 = tl.token0(t);
             if (t0 < wt.hi_max && (t0 + K8_TILE > wt.lo_min || t0 < a.sinks)) consume(t, *b, std::true_type{}); // (else the wave's rows see nothing of it)
         }
-        for (; u < n; u++) consume(tile_at(u), *turn(u), std::false_type{});
+        for (; u < n; u++) consume(tile_at(u), *turn(u, std::false_type{}), std::false_type{});
     }
     // lane (qi, grp) holds dimensions VB (4 grp + r) .. + VB of its row in o[..][r]
     const bool wide = kv8_wide(a.out, a.o_row, a.o_head, a.dtype);
@@ -1135,7 +1208,9 @@ static Kv8Plan kv8_plan(const Kv8View &c, const Kv8Rows &rw, const Kv8Attn &a, i
     const int64_t tokens = a.window ? std::min<int64_t>((int64_t)a.window + a.sinks + max_rows, (int64_t)a.max_len + max_rows) : (int64_t)a.max_len + max_rows;
     const int64_t tiles = (tokens + K8_TILE - 1) / K8_TILE;
     const int64_t one = (int64_t)a.total_rows * a.n_heads * (c.hd + 4) * sizeof(float); // workspace of a split
-    if (R <= 32) {
+    // Up to 32 product rows a block streams a share of the cache past them, and shares may join; more are worth widening tiles once for 128
+    // of them: STREAM_VS_TILES.  (2^24 rows: units fit the deal.)
+    if (R <= 32 && (int64_t)a.total_rows * c.kv_heads <= 1 << 24) {
         p.kernel = KV8_STREAM, p.mt = R <= 16 ? 1 : 2, p.max_m = R;
         const int64_t units = (int64_t)rw.n * c.kv_heads;
         // the blocks that 256 compute units hold at once; a unit in about as many parts as there are blocks for it (twice that, and one
@@ -1143,13 +1218,13 @@ static Kv8Plan kv8_plan(const Kv8View &c, const Kv8Rows &rw, const Kv8Attn &a, i
         p.goal = 256 * (p.mt == 1 ? 3 : 2);
         p.splits = tiles <= K8_MIN_TILES ? 1 : (int)std::min<int64_t>(K8_MAX_SPLITS, 2 + 2 * ((p.goal + units - 1) / units));
         if (ws_bytes >= 0) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(p.splits, ws_bytes / one));
-        p.blocks = p.goal + units;
+        p.blocks = p.splits > 1 ? p.goal + std::min<int64_t>(units, 2 * p.goal) : units; // (with more units than that kv8_deal makes at most `goal` stretches)
     } else {
         p.kernel = KV8_TILES, p.mt = 2;
         const int64_t set = 64 * p.mt, goal = 512;
         p.blocks = (rw.row_start ? a.total_rows * grps / set + rw.n : rw.n * ((R + set - 1) / set)) * c.kv_heads;
         // a split takes K8_MIN_TILES tiles at least and the context K8_MAX_SPLITS splits at most
-        p.per = (int)std::max(std::max<int64_t>((tiles * p.blocks + goal - 1) / goal, (tiles + K8_MAX_SPLITS - 1) / K8_MAX_SPLITS), (int64_t)K8_MIN_TILES);
+        p.per = (int)std::max(std::min(tiles, std::max((tiles * p.blocks + goal - 1) / goal, (tiles + K8_MAX_SPLITS - 1) / K8_MAX_SPLITS)), (int64_t)K8_MIN_TILES);
         p.splits = (int)std::max<int64_t>(1, (tiles + p.per - 1) / p.per);
         if (ws_bytes >= 0) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(p.splits, ws_bytes / one));
     }

@@ -37,14 +37,21 @@ struct Kv8Seq {
 __device__ __forceinline__ int kv8_length(int len) { return min(max(len, -KV8_MAX_TOKENS), KV8_MAX_TOKENS); }
 __device__ __forceinline__ int kv8_capacity(const Kv8View &c, int b) { return min(c.cap[b], KV8_MAX_TOKENS); }
 
+// Rows of sequence j, inside the call's rows whatever row_start holds.
+__device__ __forceinline__ int kv8_first_row(const Kv8Rows &rw, int j) { return rw.row_start ? min(max(rw.row_start[j], 0), rw.rows) : j * rw.rows; }
+__device__ __forceinline__ int kv8_last_row(const Kv8Rows &rw, int j)
+{
+    return rw.row_start ? max(min(rw.row_start[j + 1], rw.rows), kv8_first_row(rw, j)) : (j + 1) * rw.rows;
+}
+
 // uniform over the wave (every lane calls it)
 __device__ __forceinline__ Kv8Seq kv8_seq(const Kv8View &c, const Kv8Rows &rw, int j)
 {
     Kv8Seq s;
     s.b = rw.seq_ids ? rw.seq_ids[j * rw.group] : j;
     if (s.b < 0 || s.b >= c.n_seq) s.b = -1;
-    s.row0 = rw.row_start ? rw.row_start[j] : j * rw.rows;
-    s.n_rows = rw.row_start ? rw.row_start[j + 1] - s.row0 : rw.rows;
+    s.row0 = kv8_first_row(rw, j);
+    s.n_rows = kv8_last_row(rw, j) - s.row0;
     s.len = s.b < 0 ? 0 : kv8_length(rw.len[rw.path ? j * rw.group : s.b]);
     if (rw.path) {
         int t = 0;

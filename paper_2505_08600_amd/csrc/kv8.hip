@@ -461,7 +461,7 @@ static int check_attn(const char *who, const sd_kv8 *c, const sd_kv8_attn *a)
     if ((int64_t)a->rows * (a->n_heads / c->n_kv_heads) > 0x7fffffff)
         return sd_fail(SD_EINVAL, std::string(who) + ": rows times query heads per cache head must fit 31 bits");
     if (a->max_rows < 0 || a->max_len < 0) return sd_fail(SD_EINVAL, std::string(who) + ": max_rows and max_len must not be negative");
-    if (!std::isfinite(a->scale)) return sd_fail(SD_EINVAL, std::string(who) + ": scale must be finite");
+    if (!std::isfinite(a->scale * 1.44269504088896341f)) return sd_fail(SD_EINVAL, std::string(who) + ": scale must be finite");
     if (a->window < 0 || a->sinks < 0) return sd_fail(SD_EINVAL, std::string(who) + ": window and sinks must not be negative");
     if (a->sinks && !a->window) return sd_fail(SD_EINVAL, std::string(who) + ": sinks need a window");
     if (a->window && !a->causal) return sd_fail(SD_EINVAL, std::string(who) + ": a window needs causal rows");

@@ -214,7 +214,12 @@ static size_t attn_part_floats(const sd_model_config &c) { return (size_t)3072 *
 hipError_t set_rope_table(sd_model *m, const double *theta, double gain)
 {
     const int half = m->cfg.head_dim / 2, max_pos = m->cfg.max_pos;
-    std::vector<float2> tab((size_t)max_pos * half);
+    std::vector<float2> tab;
+    try {
+        tab.resize((size_t)max_pos * half);
+    } catch (const std::bad_alloc &) {
+        return hipErrorOutOfMemory;
+    }
     for (int i = 0; i < half; i++)
         for (int p = 0; p < max_pos; p++) {
             double a = p * theta[i];
@@ -555,7 +560,8 @@ extern "C" int sd_ctx_set_adapters(sd_ctx *c, sd_model *m, const int32_t *adapte
 extern "C" int sd_ctx_attach(sd_ctx *c, sd_model *m)
 {
     if (!c || !m) return sd_fail(SD_EINVAL, "sd_ctx_attach: null argument");
-    if (find_slot(c, m) >= 0) return SD_OK;
+    const int at = find_slot(c, m);
+    if (at >= 0) return c->kv8[at] ? sd_fail(SD_EINVAL, "sd_ctx_attach: model attached already with its cache in 8 bits") : SD_OK;
     if (c->n_slots >= SD_MAX_SLOTS) return sd_fail(SD_ECAP, "sd_ctx_attach: too many models");
     size_t bytes = (size_t)m->cfg.n_layers * m->cfg.d_model * c->total_cap * m->esz;
     void *k = nullptr, *v = nullptr;

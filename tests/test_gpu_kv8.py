@@ -327,6 +327,109 @@ def test_long_contexts_split_or_not(dtype, heads, kv, dim, length, rows, window,
         assert api.lib().sd_kv8_attend(api.C.byref(cache.c), api.C.byref(a), api._stream()) == api.SD_ECAP
 
 
+KINDS = [(2, 2, 64, 6), (2, 2, 128, 6), (4, 1, 128, 5), (4, 1, 64, 7), (2, 1, 128, 40), (3, 3, 64, 70), (2, 1, 48, 9)]  # heads, cache heads, dim, rows
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("heads,kv,dim,rows", KINDS)
+def test_rows_of_very_different_size(dtype, heads, kv, dim, rows):
+    """A row's precision is that of its own elements, whatever the rows beside it hold."""
+    ref = kv8ref.Cache([400], kv, dim).fill(dim)
+    q = torch.randn(rows, heads, dim, generator=torch.Generator().manual_seed(rows))
+    for i, f in ((1, 1e6), (2, 1e-3), (3, 1e30), (4, 1e12), (6, 1e-25), (33, 1e5), (36, 1e35)):
+        q[i:i + 1] *= f
+    q = q.to(dtype)
+    for scale in (dim ** -0.5, -0.2):
+        close(run_attend(ref.to_gpu(), q, [330], [rows], scale), kv8ref.attend(ref, q, [(0, 330, 0, rows)], scale))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("heads,kv,dim,rows", KINDS)
+@pytest.mark.parametrize("length", [330, 1])
+def test_queries_that_are_not_numbers(dtype, heads, kv, dim, rows, length):
+    """A NaN or an infinity makes its own row and head NaN and no other; a row that sees nothing stays zeros."""
+    ref = kv8ref.Cache([length + rows, 1], kv, dim).fill(dim)
+    q = torch.randn(2 * rows, heads, dim, generator=torch.Generator().manual_seed(rows))
+    good = q.clone()
+    bad = torch.zeros(2 * rows, heads, dtype=torch.bool)
+    for r, h, d, x in ((1, 0, 5, math.nan), (3, heads - 1, dim - 1, math.inf), (4, 0, 0, -math.inf), (rows - 1, 1, dim // 2, math.nan)):
+        q[r, h, d], bad[r, h] = x, True
+    q[rows:, :, 3] = math.nan
+    q, good = q.to(dtype), good.to(dtype)
+    out, lse = run_attend(ref.to_gpu(), q, [length, 0], [rows, rows], 0.1, causal=False, ragged=False)
+    assert (out[rows:] == 0).all() and (lse[rows:] == -math.inf).all()
+    assert torch.isnan(out[bad]).all() and torch.isnan(lse[bad]).all()
+    want = kv8ref.attend(ref, good, [(0, length, 0, rows), (1, 0, rows, rows)], 0.1, causal=False)
+    live = ~bad
+    live[rows:] = False
+    close((out[live], lse[live]), tuple(t[live] for t in want))
+
+
+@pytest.mark.parametrize("rows,max_rows", [(3, 3), (3, 1), (1, 60), (40, 1), (40, 40)])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_many_sequences(dim, rows, max_rows):
+    """150 of them, short and long, in another order, some with no row, one id out of range; max_rows right, too small, too large."""
+    rng = np.random.default_rng(rows)
+    n = 150
+    lens = [int(x) for x in rng.integers(0, 90, n)]
+    lens[77], lens[140] = 2500, 1300
+    ref = kv8ref.Cache([x + rows for x in lens], 2, dim).fill(4)
+    ids = [int(x) for x in rng.permutation(n)]
+    counts = [int(x) for x in rng.integers(0, rows + 1, n)]
+    for b in (77, 140):
+        counts[ids.index(b)] = rows
+    lost = ids.index(5)
+    counts[lost], ids[lost] = 1, n + 3
+    first = starts(counts).tolist()
+    q = torch.randn(first[-1], 4, dim, generator=torch.Generator().manual_seed(rows)).to(BF16)
+    cache = ref.to_gpu()
+    qd, out, lse = q.cuda(), torch.full_like(q, 3.0).cuda(), torch.zeros(first[-1], 4).cuda()
+    api.sd_kv8_attend(cache, i32(*lens).cuda(), qd, out, 0.1, row_start=starts(counts).cuda(), max_rows=max_rows, max_len=2500, lse=lse, seq_ids=i32(*ids).cuda())
+    assert cache.status.item() == 4
+    out, lse = out.cpu(), lse.cpu()
+    assert (out[first[lost]] == 3.0).all()
+    parts = [(b, lens[b], first[j], counts[j]) for j, b in enumerate(ids) if b < n and (rows < 10 or j % 9 == 0 or b in (77, 140))]
+    live = [r for _, _, r0, m in parts for r in range(r0, r0 + m)]
+    close((out[live], lse[live]), tuple(t[live] for t in kv8ref.attend(ref, q, parts, 0.1)))
+
+
+@pytest.mark.parametrize("workspace", [True, False])
+def test_one_long_context_among_very_many(workspace):
+    """A million tokens beside 65535 short sequences: the tiles of all, each as long as the longest, would not fit 31 bits."""
+    n, long = 65536, 1 << 20
+    lens = torch.arange(n, dtype=torch.int32) % 3
+    at = 40_000
+    lens[at] = long - 1
+    ref = kv8ref.Cache((lens + 1).tolist(), 1, 64).fill(6)
+    cache = ref.to_gpu()
+    q = torch.randn(n, 1, 64, generator=torch.Generator().manual_seed(1))
+    qd, out, lse = q.cuda(), torch.full_like(q, math.nan).cuda(), torch.full((n, 1), math.nan).cuda()
+    if workspace:
+        api.sd_kv8_attend(cache, lens.cuda(), qd, out, 0.1, max_len=long - 1, lse=lse)
+    else:
+        ld = lens.cuda()
+        a = api._Kv8Attn(None, ld.data_ptr(), None, n, n, 1, 0, 1, api.SD_FP32, *api._rows3(qd, "q"), *api._rows3(out, "out"), lse.data_ptr(), 0.1,
+                         1, 0, 0, None, 0)
+        api._check(api.lib().sd_kv8_attend(api.C.byref(cache.c), api.C.byref(a), api._stream()))
+    out, lse = out.cpu(), lse.cpu()
+    assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+    some = [0, 1, 2, 64, 127, at - 1, at, at + 1, n - 1]
+    want = kv8ref.attend(ref, q, [(b, int(lens[b]), b, 1) for b in some], 0.1)
+    close((out[some], lse[some]), tuple(t[some] for t in want))
+
+
+def test_row_starts_behind_the_rows():
+    """Rows that row_start gives a sequence beyond the call's rows are not touched."""
+    ref = kv8ref.Cache([100, 100], 1, 64).fill(3)
+    q = torch.randn(6, 1, 64, generator=torch.Generator().manual_seed(1))
+    for max_rows in (2, 60):
+        out = torch.full((40, 1, 64), 3.0).cuda()
+        api.sd_kv8_attend(ref.to_gpu(), i32(40, 50).cuda(), q.cuda(), out[:6], 0.1, row_start=i32(0, 4, 100_000).cuda(), max_rows=max_rows, max_len=50)
+        assert (out[6:] == 3.0).all()
+        want, _, bound, _ = kv8ref.attend(ref, q, [(0, 40, 0, 4), (1, 50, 4, 2)], 0.1)
+        assert ((out[:6].cpu().double() - want).abs() <= bound).all()
+
+
 def test_plain_kernel_agrees():
     """Option force_generic = 2 (attention): the plain kernel, within the same bounds."""
     ref = kv8ref.Cache([300], 2, 128).fill(2)
@@ -514,7 +617,7 @@ def test_attach_and_cache_rows():
     ctx.attach_kv8(m)                                     # the same form again: fine
     plain.attach(m)
     for bad in (lambda: ctx.attach_kv8(m, 8), lambda: plain.attach_kv8(m), lambda: api.Context([64]).attach_kv8(m, 0, 3),
-                lambda: api.Context([64]).attach_kv8(m, -1)):
+                lambda: api.Context([64]).attach_kv8(m, -1), lambda: ctx.attach(m)):
         with pytest.raises(api.SdError):
             bad()
     rows = [dg.f32_to_bf16_bits(np.random.default_rng(k).standard_normal((50, shape.n_heads, shape.head_dim)).astype(np.float32)) for k in range(2)]

@@ -117,6 +117,22 @@ def test_refused_attention():
     assert L.sd_kv8_attend_workspace(C.byref(cache()), C.byref(attn())) >= 0
 
 
+def test_scales_that_leave_the_range():
+    assert L.sd_kv8_attend(C.byref(cache()), C.byref(attn(scale=3e38)), None) == api.SD_EINVAL   # times log2(e)
+    assert L.sd_kv8_attend(C.byref(cache()), C.byref(attn(scale=-3e38)), None) == api.SD_EINVAL
+
+
+@pytest.mark.parametrize("rows", [1 << 23, 4096, 2])
+@pytest.mark.parametrize("max_rows", [0, 1, 2 ** 31 - 1])
+@pytest.mark.parametrize("window", [0, 100, 2 ** 31 - 1])
+def test_workspace_of_the_longest_contexts(rows, max_rows, window):
+    """At most 64 parts of every row, whatever the lengths."""
+    a = attn(rows=rows, row_start=GOOD, max_rows=max_rows, max_len=2 ** 31 - 1, window=window)
+    need = L.sd_kv8_attend_workspace(C.byref(cache(tokens=2 ** 40)), C.byref(a))
+    one = rows * 4 * (64 + 4) * 4
+    assert 0 <= need <= 64 * one and need % one == 0
+
+
 def test_refused_contexts():
     assert L.sd_ctx_attach_kv8(None, None, 0, 0) == api.SD_EINVAL
     assert L.sd_ctx_get_kv(None, None, 0, 0, None, None, 1) == api.SD_EINVAL
