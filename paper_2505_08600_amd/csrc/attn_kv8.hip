@@ -145,7 +145,12 @@ typedef __attribute__((ext_vector_type(4))) float f32x4;
 
 #define K8_TILE 32
 #define K8_UNIT_COST 8   // tiles whose time a unit's start and end take
-#define K8_MIN_TILES 16  // tiles of a split at least
+// Few rows: contexts of up to K8_WHOLE tiles are not split (a token in 1024 of 8 heads of 128: 14.5 us in parts and joined, 13.4 whole; 32 times
+// that with 32 heads 64.7 and 59.3; but one in 1536 tokens 16.0 and 17.7), parts of longer ones have K8_MIN_TILES at least (one in 2048
+// tokens: 16.6 us in parts of 16 tiles, 13.2 in parts of 8).
+#define K8_WHOLE 40
+#define K8_MIN_TILES 8
+#define K8_MIN_SPLIT 16  // many rows: tiles of a split at least
 #define K8_MAX_SPLITS 64 // splits of a context at most
 #define K8_P_SHIFT 14 // probabilities enter as p * (vs / E) * 2^14 < 2^15
 
@@ -1216,15 +1221,15 @@ static Kv8Plan kv8_plan(const Kv8View &c, const Kv8Rows &rw, const Kv8Attn &a, i
         // the blocks that 256 compute units hold at once; a unit in about as many parts as there are blocks for it (twice that, and one
         // more at either end, where lengths differ)
         p.goal = 256 * (p.mt == 1 ? 3 : 2);
-        p.splits = tiles <= K8_MIN_TILES ? 1 : (int)std::min<int64_t>(K8_MAX_SPLITS, 2 + 2 * ((p.goal + units - 1) / units));
+        p.splits = tiles <= K8_WHOLE ? 1 : (int)std::min<int64_t>(K8_MAX_SPLITS, 2 + 2 * ((p.goal + units - 1) / units));
         if (ws_bytes >= 0) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(p.splits, ws_bytes / one));
         p.blocks = p.splits > 1 ? p.goal + std::min<int64_t>(units, 2 * p.goal) : units; // (with more units than that kv8_deal makes at most `goal` stretches)
     } else {
         p.kernel = KV8_TILES, p.mt = 2;
         const int64_t set = 64 * p.mt, goal = 512;
         p.blocks = (rw.row_start ? a.total_rows * grps / set + rw.n : rw.n * ((R + set - 1) / set)) * c.kv_heads;
-        // a split takes K8_MIN_TILES tiles at least and the context K8_MAX_SPLITS splits at most
-        p.per = (int)std::max(std::min(tiles, std::max((tiles * p.blocks + goal - 1) / goal, (tiles + K8_MAX_SPLITS - 1) / K8_MAX_SPLITS)), (int64_t)K8_MIN_TILES);
+        // a split takes K8_MIN_SPLIT tiles at least and the context K8_MAX_SPLITS splits at most
+        p.per = (int)std::max(std::min(tiles, std::max((tiles * p.blocks + goal - 1) / goal, (tiles + K8_MAX_SPLITS - 1) / K8_MAX_SPLITS)), (int64_t)K8_MIN_SPLIT);
         p.splits = (int)std::max<int64_t>(1, (tiles + p.per - 1) / p.per);
         if (ws_bytes >= 0) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(p.splits, ws_bytes / one));
     }
