@@ -540,6 +540,7 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void kv8_attn_stream_kernel(K
         const int u0 = f.start + unit * f.len; // the unit's first position
         const int t_begin = (at - u0) << deal.grain, first_blk = (unsigned)u0 / (unsigned)deal.chunk, split = blk - first_blk;
         const bool only = u0 + f.len <= (first_blk + 1) * deal.chunk; // the whole unit is this block's
+        const int parts = split ? 0 : (unsigned)(u0 + f.len - 1) / (unsigned)deal.chunk - first_blk + 1; // what the unit ends up in
         const int set = (unsigned)unit / (unsigned)c.kv_heads, kvh = unit - set * c.kv_heads, m0 = set * SET;
         const int n_here = max(1, min(end, u0 + f.len) - at); // (always one: should rows overlap, which row_start must not say, the loop still ends)
         at += n_here;
@@ -785,11 +786,12 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void kv8_attn_stream_kernel(K
                 for (int d = 0; d < VB; d++) v[d] = i >= n_rows ? 0.f : v[d] * g;
                 kv8_store_run<VB>(a, kv8_wide(a.out, a.o_row, a.o_head, a.dtype), r, h, HD, d0, v);
                 if (a.lse && d0 == 0) a.lse[(int64_t)r * a.n_heads + h] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
+                if (S > 1 && d0 == 0) part[((int64_t)r * a.n_heads + h) * S * (HD + 4) + 2] = __uint_as_float(1); // (nothing to join)
             } else if ((unsigned)split < (unsigned)S) { // (always, but for such rows)
                 float *p = part + (((int64_t)r * a.n_heads + h) * S + split) * (HD + 4);
 #pragma unroll
                 for (int d = 0; d < VB; d += 4) *(float4 *)(p + 4 + d0 + d) = make_float4(v[d], v[d + 1], v[d + 2], v[d + 3]);
-                if (d0 == 0) p[0] = M, p[1] = L;
+                if (d0 == 0) *(float4 *)p = make_float4(M, L, __uint_as_float(parts), 0.f);
             }
         }
     }
@@ -1131,7 +1133,7 @@ __global__ __launch_bounds__(256, 3) void kv8_attn_tile_kernel(Kv8View c, Kv8Row
 }
 
 // ---------------------------------------------------------------- parts of a context meet
-// HD / 4 threads per product row; parts lie one after the other, { maximum, sum, -, -, HD outputs } each.
+// HD / 4 threads per product row; parts lie one after the other, { maximum, sum, number of parts (in the first one), -, HD outputs } each.
 template <int HD>
 __device__ __forceinline__ void kv8_join_row(const Kv8Attn &a, int r, int h, int used, int S, const float *part)
 {
@@ -1156,27 +1158,19 @@ __device__ __forceinline__ void kv8_join_row(const Kv8Attn &a, int r, int h, int
     if (a.lse && dg == 0) a.lse[(int64_t)r * a.n_heads + h] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
 }
 
-// Of kv8_attn_stream_kernel<HD, SET / 16, ..>: a block takes 1024 / HD product rows of one (sequence, cache head) at a time.
-template <int HD, int SET>
-__global__ __launch_bounds__(256) void kv8_attn_join_kernel(Kv8View c, Kv8Rows rw, Kv8Attn a, int n_groups, int S, int goal, const float *__restrict__ part)
+// Of kv8_attn_stream_kernel<HD, ..>: a block takes 1024 / HD product rows of one (sequence, cache head) at a time.
+template <int HD>
+__global__ __launch_bounds__(256) void kv8_attn_join_kernel(Kv8View c, Kv8Rows rw, Kv8Attn a, int n_groups, int S, const float *__restrict__ part)
 {
     constexpr int NG = 1024 / HD;
     const int kvh = blockIdx.x % c.kv_heads, j = blockIdx.x / c.kv_heads % rw.n, g0 = blockIdx.x / c.kv_heads / rw.n;
-    const Kv8Deal deal = kv8_deal<SET>(c, rw, a, S, goal);
-    int u0 = 0, T = 0; // where the sequence's units start, and their tiles
-    for (int k = threadIdx.x & 63, first = 1; k - (int)(threadIdx.x & 63) <= j; k += 64, first = 0) {
-        const Kv8Units u = first ? deal.mine : kv8_units<SET>(c, rw, a, k);
-        u0 += k < j ? deal.length(u.T) * u.n : 0;
-        T += k == j ? u.T : 0;
-    }
-    u0 = wave_total(u0), T = wave_total(T);
-    if (T == 0) return;
     const Kv8Seq sq = kv8_seq(c, rw, j);
-    const int grps = a.n_heads / c.kv_heads, len = deal.length(T);
+    if (sq.b < 0) return;
+    const int grps = a.n_heads / c.kv_heads;
     for (int m = g0 * NG + threadIdx.x / (HD / 4); m < sq.n_rows * grps; m += n_groups * NG) {
-        const int at = u0 + (m / SET * c.kv_heads + kvh) * len;
-        const int used = (unsigned)(at + len - 1) / (unsigned)deal.chunk - (unsigned)at / (unsigned)deal.chunk + 1, i = (unsigned)m / (unsigned)grps;
-        if (used > 1) kv8_join_row<HD>(a, sq.row0 + i, kvh * grps + (m - i * grps), used, S, part); // (else the result is there)
+        const int i = (unsigned)m / (unsigned)grps, r = sq.row0 + i, h = kvh * grps + (m - i * grps);
+        const int used = min((int)__float_as_uint(part[((int64_t)r * a.n_heads + h) * S * (HD + 4) + 2]), S);
+        if (used > 1) kv8_join_row<HD>(a, r, h, used, S, part); // (else the result is there)
     }
 }
 
@@ -1253,8 +1247,8 @@ static hipError_t mfma_launch(hipStream_t s, const Kv8Plan &p, const Kv8View &c,
         hipLaunchKernelGGL((kv8_attn_stream_kernel<HD, MT, T>), dim3((unsigned)p.blocks), dim3(256), 0, s, c, rw, a, p.splits, p.goal, part);      \
         if (p.splits > 1) {                                                                                                                      \
             const int groups = (int)((p.max_m + NG - 1) / NG);                                                                                   \
-            hipLaunchKernelGGL((kv8_attn_join_kernel<HD, 16 * MT>), dim3((unsigned)((int64_t)rw.n * c.kv_heads * groups)), dim3(256), 0, s, c, rw, a, \
-                               groups, p.splits, p.goal, part);                                                                                  \
+            hipLaunchKernelGGL(kv8_attn_join_kernel<HD>, dim3((unsigned)((int64_t)rw.n * c.kv_heads * groups)), dim3(256), 0, s, c, rw, a, groups,  \
+                               p.splits, part);                                                                                  \
         }                                                                                                                                        \
     } while (0)
 #define TILES(T) hipLaunchKernelGGL((kv8_attn_tile_kernel<HD, 2, T>), dim3((unsigned)p.blocks, p.splits), dim3(256), 0, s, c, rw, a, p.splits, p.per, part)

@@ -418,6 +418,31 @@ def test_one_long_context_among_very_many(workspace):
     close((out[some], lse[some]), tuple(t[some] for t in want))
 
 
+@pytest.mark.parametrize("rows,dim", [(3, 128), (5, 64), (100, 128)])
+def test_workspace_contents_do_not_matter(rows, dim):
+    lens = [4000, 30, 1500]
+    ref = kv8ref.Cache([x + rows for x in lens], 2, dim).fill(3)
+    cache, ld = ref.to_gpu(), i32(*lens).cuda()
+    q = torch.randn(3 * rows, 4, dim, generator=torch.Generator().manual_seed(1)).cuda()
+    first = None
+    for fill in (0, 1, 127, 255):
+        out, lse = torch.zeros_like(q), torch.zeros(3 * rows, 4).cuda()
+        a = api._Kv8Attn(None, ld.data_ptr(), None, 3, 3 * rows, 0, max(lens), 4, api.SD_FP32, *api._rows3(q, "q"), *api._rows3(out, "out"), lse.data_ptr(),
+                         0.1, 1, 0, 0, None, 0)
+        need = api.lib().sd_kv8_attend_workspace(api.C.byref(cache.c), api.C.byref(a))
+        assert need > 0
+        ws = torch.full((need + 4096,), fill, dtype=torch.uint8).cuda()
+        a.workspace, a.workspace_bytes = ws.data_ptr(), need
+        api._check(api.lib().sd_kv8_attend(api.C.byref(cache.c), api.C.byref(a), api._stream()))
+        assert (ws[need:] == fill).all()
+        first = first or (out, lse)
+        assert torch.equal(out, first[0]) and torch.equal(lse, first[1])
+    show = [0, rows - 1]
+    want = kv8ref.attend(ref, q.cpu(), [(b, lens[b] + i, b * rows + i, 1) for b in range(3) for i in show], 0.1)
+    live = [b * rows + i for b in range(3) for i in show]
+    close((first[0].cpu()[live], first[1].cpu()[live]), tuple(t[live] for t in want))
+
+
 def test_row_starts_behind_the_rows():
     """Rows that row_start gives a sequence beyond the call's rows are not touched."""
     ref = kv8ref.Cache([100, 100], 1, 64).fill(3)
