@@ -422,8 +422,9 @@ __device__ __forceinline__ Kv8Deal kv8_deal(const Kv8View &c, const Kv8Rows &rw,
     int T_max = max(1, d.mine.T);
     for (int j = lane + 64; j - lane < rw.n; j += 64) T_max = max(T_max, kv8_units<SET>(c, rw, a, j).T);
     T_max = wave_most(T_max);
-    // at most `units` of them (2^24: kv8_plan), so that 2^29 positions hold all and the longest is no longer than 2^18
-    const uint64_t units = (uint64_t)(unsigned)a.total_rows * (unsigned)c.kv_heads, most = units * (unsigned)(T_max + K8_UNIT_COST) >> 29 | (unsigned)T_max >> 18;
+    // at most `units` of them (two for a row and cache head; 2^25: kv8_plan), so that 2^29 positions hold all and the longest is no longer
+    // than 2^18
+    const uint64_t units = (uint64_t)(unsigned)a.total_rows * (unsigned)c.kv_heads * 2, most = units * (unsigned)(T_max + K8_UNIT_COST) >> 29 | (unsigned)T_max >> 18;
     d.grain = most ? 64 - __builtin_clzll(most) : 0;
     T_max = (T_max + (1 << d.grain) - 1) >> d.grain;
     d.cross = true;
@@ -509,7 +510,7 @@ struct K8Regs {
     float sc; // lanes 0..31: the K scale of the tile's token of that number, lanes 32..63: V scales
 };
 
-// Block: 4 waves over the tiles of one (sequence, cache head, set of MT * 16 rows, split), each with a running softmax of its own.
+// Block: 4 waves over its stretch of the tiles of (sequence, cache head, set of MT * 16 rows) units, each with a running softmax of its own.
 //   S^T = K Q^T in integers: two operands of 16 tokens each are the codes' rows as they lie, in 16-byte pieces; the queries are three
 //   signed bytes.  The result leaves lane (qi, grp)
 //   tokens 4 grp + r of both halves for row qi, which are the eight k-slots of the P^T operand of
@@ -747,7 +748,7 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void kv8_attn_stream_kernel(K
         }
         // the waves' parts meet: O in true units (E and the shifts undone), weighted by their maxima.  Thread (row, c) of the sum holds
         // VB adjacent dimensions of a row.
-        const float back = E * 0.03125f; // 2^(9 - 14)
+        const float back = E * pow2(9 - K8_P_SHIFT); // (V's halves are codes * 2^-9)
         const int row = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * VB;
 #pragma unroll
         for (int mt = 0; mt < MT; mt++) {
@@ -809,7 +810,7 @@ __global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void kv8_attn_stream_kernel(K
 #define K8_LAZY 4.0f
 #define K8_P_SHIFT_LAZY 10 // p * (vs / E) * 2^10 < 2^15
 template <int HD, int MT, int TERMS>
-__global__ __launch_bounds__(256, 3) void kv8_attn_tile_kernel(Kv8View c, Kv8Rows rw, Kv8Attn a, int S, int per_want, float *part)
+__global__ __launch_bounds__(256, MT == 1 ? 4 : 3) void kv8_attn_tile_kernel(Kv8View c, Kv8Rows rw, Kv8Attn a, int S, int per_want, float *part)
 {
     constexpr int NS = HD / 32, VB = HD / 16, ND = VB, NF = 2 * NS + ND; // fragments of a tile: K's, then V's
     constexpr int ROWS = 4 * MT * 16;
@@ -1098,7 +1099,7 @@ __global__ __launch_bounds__(256, 3) void kv8_attn_tile_kernel(Kv8View c, Kv8Row
     }
     // lane (qi, grp) holds dimensions VB (4 grp + r) .. + VB of its row in o[..][r]
     const bool wide = kv8_wide(a.out, a.o_row, a.o_head, a.dtype);
-    const float unit = E * (K8_P_SHIFT_LAZY == 10 ? 0.5f : 0.f); // 2^(9 - 10)
+    const float unit = E * pow2(9 - K8_P_SHIFT_LAZY); // (V's halves are codes * 2^-9)
 #pragma unroll
     for (int mt = 0; mt < MT; mt++) {
         const float l = rows4_sum(l_run[mt]);
@@ -1174,11 +1175,11 @@ __global__ __launch_bounds__(256) void kv8_attn_join_kernel(Kv8View c, Kv8Rows r
     }
 }
 
-// Of kv8_attn_tile_kernel<HD, 2, ..>: 1024 / HD (row, head) pairs per block.
-template <int HD>
+// Of kv8_attn_tile_kernel<HD, SET / 64, ..>: 1024 / HD (row, head) pairs per block.
+template <int HD, int SET>
 __global__ __launch_bounds__(256) void kv8_attn_join_tiles_kernel(Kv8View c, Kv8Rows rw, Kv8Attn a, int S, int per_want, const float *__restrict__ part)
 {
-    constexpr int NG = 1024 / HD, SET = 128;
+    constexpr int NG = 1024 / HD;
     const int r = blockIdx.x, h = blockIdx.y * NG + threadIdx.x / (HD / 4);
     const int j = kv8_owner(rw, r);
     if (j < 0 || j >= rw.n) return;
@@ -1207,11 +1208,13 @@ static Kv8Plan kv8_plan(const Kv8View &c, const Kv8Rows &rw, const Kv8Attn &a, i
     const int64_t tokens = a.window ? std::min<int64_t>((int64_t)a.window + a.sinks + max_rows, (int64_t)a.max_len + max_rows) : (int64_t)a.max_len + max_rows;
     const int64_t tiles = (tokens + K8_TILE - 1) / K8_TILE;
     const int64_t one = (int64_t)a.total_rows * a.n_heads * (c.hd + 4) * sizeof(float); // workspace of a split
-    // Up to 32 product rows a block streams a share of the cache past them, and shares may join; more are worth widening tiles once for 128
-    // of them: STREAM_VS_TILES.  (2^24 rows: units fit the deal.)
-    if (R <= 32 && (int64_t)a.total_rows * c.kv_heads <= 1 << 24) {
+    // Up to 64 product rows blocks stream the cache past 16 or 32 of them, more are worth widening tiles once for all rows of a block.  Streaming
+    // and tiles, 16 sequences of 4096 tokens, 8 heads of 128, bf16 (fp32): 32 rows 44 and 60 us (47, 55), 64 rows 54 and 64 (57, 59), 96 rows
+    // 102 and 70 (107, 95); one such sequence: 32 rows 17 and 29 (18, 26), 64 rows 21 and 30 (23, 28), 128 rows 28 and 32 (30, 29).
+    // (2^24: the units fit the deal.)
+    if (R <= 64 && (int64_t)a.total_rows * c.kv_heads <= 1 << 24) {
         p.kernel = KV8_STREAM, p.mt = R <= 16 ? 1 : 2, p.max_m = R;
-        const int64_t units = (int64_t)rw.n * c.kv_heads;
+        const int64_t units = (int64_t)rw.n * c.kv_heads * ((R + 16 * p.mt - 1) / (16 * p.mt));
         // the blocks that 256 compute units hold at once; a unit in about as many parts as there are blocks for it (twice that, and one
         // more at either end, where lengths differ)
         p.goal = 256 * (p.mt == 1 ? 3 : 2);
@@ -1219,7 +1222,9 @@ static Kv8Plan kv8_plan(const Kv8View &c, const Kv8Rows &rw, const Kv8Attn &a, i
         if (ws_bytes >= 0) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(p.splits, ws_bytes / one));
         p.blocks = p.splits > 1 ? p.goal + std::min<int64_t>(units, 2 * p.goal) : units; // (with more units than that kv8_deal makes at most `goal` stretches)
     } else {
-        p.kernel = KV8_TILES, p.mt = 2;
+        // (two 16-row sets a wave share an operand read from LDS; two terms of everything leave registers for one: 4096 fp32 rows of 32 heads over
+        // 8 of 128 450 us with two, 278 with one)
+        p.kernel = KV8_TILES, p.mt = a.dtype == SD_BF16 ? 2 : 1;
         const int64_t set = 64 * p.mt, goal = 512;
         p.blocks = (rw.row_start ? a.total_rows * grps / set + rw.n : rw.n * ((R + set - 1) / set)) * c.kv_heads;
         // a split takes K8_MIN_SPLIT tiles at least and the context K8_MAX_SPLITS splits at most
@@ -1251,12 +1256,16 @@ static hipError_t mfma_launch(hipStream_t s, const Kv8Plan &p, const Kv8View &c,
                                p.splits, part);                                                                                  \
         }                                                                                                                                        \
     } while (0)
-#define TILES(T) hipLaunchKernelGGL((kv8_attn_tile_kernel<HD, 2, T>), dim3((unsigned)p.blocks, p.splits), dim3(256), 0, s, c, rw, a, p.splits, p.per, part)
+#define TILES(MT, T)                                                                                                                             \
+    do {                                                                                                                                         \
+        hipLaunchKernelGGL((kv8_attn_tile_kernel<HD, MT, T>), dim3((unsigned)p.blocks, p.splits), dim3(256), 0, s, c, rw, a, p.splits, p.per, part); \
+        if (p.splits > 1)                                                                                                                        \
+            hipLaunchKernelGGL((kv8_attn_join_tiles_kernel<HD, 64 * MT>), dim3(a.total_rows, (a.n_heads + NG - 1) / NG), dim3(256), 0, s, c, rw, a, \
+                               p.splits, p.per, part);                                                                                           \
+    } while (0)
     if (p.kernel == KV8_TILES) {
-        if (bf16) TILES(1);
-        else TILES(2);
-        if (p.splits > 1)
-            hipLaunchKernelGGL(kv8_attn_join_tiles_kernel<HD>, dim3(a.total_rows, (a.n_heads + NG - 1) / NG), dim3(256), 0, s, c, rw, a, p.splits, p.per, part);
+        if (bf16) TILES(2, 1);
+        else TILES(1, 2);
     } else if (p.mt == 1) {
         if (bf16) STREAM(1, 1);
         else STREAM(1, 2);

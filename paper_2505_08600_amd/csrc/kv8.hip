@@ -168,9 +168,9 @@ __device__ __forceinline__ int64_t row_place(const Kv8View &c, const Kv8Rows &rw
     return c.off[b] + t;
 }
 
-// Both kernels: a block serves RB adjacent rows (RB > 1: and memory with the nontemporal hint).  Its first threads find the rows' places; pieces of 8 elements are then dealt out with a
-// vector's lanes innermost, then the rows, then the vectors (K and V of each head), so that the codes of adjacent tokens are
-// touched together, and four at a time per thread, so that their loads are in flight together.
+// Both kernels: a block serves RB adjacent rows (RB > 1: and memory with the nontemporal hint).  Its first threads find the rows' places;
+// pieces of 8 elements are then dealt out with a vector's lanes innermost, then the rows, then the vectors (K and V of each head), so
+// that the codes of adjacent tokens are touched together, and four at a time per thread, so that their loads are in flight together.
 template <int RB>
 struct Kv8Piece {
     int l, row, w; // lane of the vector, row of the block, vector (2 * head + (0: K, 1: V))
@@ -265,10 +265,12 @@ static bool wide_rows(int esz, const void *p, int64_t row, int64_t head)
 {
     return ((uintptr_t)p % 16) == 0 && row * esz % 16 == 0 && head * esz % 16 == 0;
 }
-// Few rows: a row per block, and its vectors spread over blocks too, so that the chip fills; many: 32 rows per block, so that a
-// block's search for its rows is paid for by more bytes (51200 rows of 8 heads of 128 read back as bf16: 92 us with one row, 77 with
-// 8 to 64).
-#define KV8_ROWS 32
+// Few bytes: a row per block, and its vectors spread over blocks too, so that the chip fills.  Many (2^23 elements of K: more than stays in
+// a cache beside what else a step touches): eight adjacent rows per block, whose codes lie together, and the nontemporal hint.  Rows of
+// 8 heads of 128, bf16: 2048 of them appended 7.3 us with one row per block, 7.9 with eight; 51200 appended 100 with one, 75 with four,
+// 71 with eight, 78 with 32, read back 90, 69, 68, 71 (fp32: 105, 99, 101, 112 and 127, 108, 115, 122).
+#define KV8_ROWS 8
+static int kv8_rows_per_block(int n_rows, const Kv8View &c) { return (int64_t)n_rows * c.kv_heads * c.hd >= 1 << 23 ? KV8_ROWS : 1; }
 static dim3 vector_grid(int n_rows, int rb, int kv_heads, int lane_bits)
 {
     const int gx = (n_rows + rb - 1) / rb, turns = ((2 * kv_heads * rb << lane_bits) + 1023) / 1024;
@@ -276,7 +278,7 @@ static dim3 vector_grid(int n_rows, int rb, int kv_heads, int lane_bits)
 }
 
 #define KV8_MOVE(KERNEL, CV)                                                                                                                   \
-    const int esz = dtype == SD_BF16 ? 2 : 4, bits = vector_lane_bits(c.hd), rb = n_rows >= 2048 ? KV8_ROWS : 1;                               \
+    const int esz = dtype == SD_BF16 ? 2 : 4, bits = vector_lane_bits(c.hd), rb = kv8_rows_per_block(n_rows, c);                               \
     const bool wide = wide_rows(esz, k, k_row, k_head) && wide_rows(esz, v, v_row, v_head); /* (a null pointer counts as aligned) */            \
     const dim3 grid = vector_grid(n_rows, rb, c.kv_heads, bits);                                                                               \
     if (dtype == SD_BF16) {                                                                                                                    \

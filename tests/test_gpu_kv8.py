@@ -245,6 +245,33 @@ def test_unseen_tokens_leave_no_trace(dtype, dim):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (45, 3)])
+def test_unseen_tokens_leave_no_trace_in_prompts(dtype, dim, window, sinks):
+    """The same with more rows: NaN scales of every token that no row sees, and of one that only the last rows see."""
+    lens, rows, heads = [150, 33], [70, 131], 2
+    clean = kv8ref.Cache([300, 300], heads, dim, gap=40).fill(11)
+    dirty = kv8ref.Cache([300, 300], heads, dim, gap=40)
+    for a, b in ((dirty.k, clean.k), (dirty.v, clean.v), (dirty.ks, clean.ks), (dirty.vs, clean.vs)):
+        a.copy_(b)
+    seen = torch.zeros(dirty.tokens, dtype=torch.bool)
+    for b in range(2):
+        for i in range(rows[b]):
+            seen[[dirty.off[b] + t for t in kv8ref.visible(lens[b], i, 300, True, window, sinks)]] = True
+    for s in (dirty.ks, dirty.vs):
+        s[:, ~seen] = math.nan
+    q = torch.randn(sum(rows), heads, dim, generator=torch.Generator().manual_seed(1)).to(dtype)
+    got = [run_attend(c.to_gpu(), q, lens, rows, 0.125, window=window, sinks=sinks) for c in (clean, dirty)]
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1]) and torch.isfinite(got[1][0]).all()
+    dirty.vs[0, dirty.off[0] + 200] = math.nan            # seen from row 50 of the first sequence on
+    dirty.ks[1, dirty.off[1] + 160] = math.nan            # seen from row 127 of the second one on
+    out, lse = run_attend(dirty.to_gpu(), q, lens, rows, 0.125, window=window, sinks=sinks)
+    last = 70 if not window else min(70, 50 + 45)
+    assert torch.isnan(out[50:last, 0]).all() and torch.equal(out[:50, 0], got[0][0][:50, 0]) and torch.equal(out[:70, 1], got[0][0][:70, 1])
+    assert torch.isnan(out[70 + 127:, 1]).all() and torch.equal(out[70:70 + 127, 1], got[0][0][70:70 + 127, 1]) and torch.equal(out[70:, 0], got[0][0][70:, 0])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 def test_strides_ids_and_rows_left_alone(dtype):
     """q inside a packed buffer, out with gaps, sequences out of order, one id out of range."""
     heads, kv, dim, lens = 4, 2, 64, [20, 90, 45]
