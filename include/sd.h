@@ -322,9 +322,11 @@ int sd_kv8_read(const sd_kv8 *c, const int32_t *seq_ids, int32_t n_seq, const in
  *     hides what lies window or more tokens back, except the first `sinks` tokens (0: the whole context; sinks is then 0 too).
  *   causal == 0: every row sees the len[b] tokens of its sequence (window 0).
  * A row that sees nothing gets zeros (and a log-sum-exp of -infinity).  Tokens a row does not see leave no trace in it,
- * whatever their memory holds.  Query head h reads cache head h / (n_heads / n_kv_heads).
- * Scores, running maxima, sums and outputs are 32-bit; queries and probabilities enter the matrix cores as 16-bit terms -
- * two each for SD_FP32 rows (22 bits), one for SD_BF16 rows (bf16 queries exactly, probabilities to 11 bits). */
+ * whatever their memory holds.  A row of q with a NaN or an infinity gives NaN in its head, and in no other row.  Query head h reads
+ * cache head h / (n_heads / n_kv_heads).  out must not overlap q.
+ * Scores, running maxima, sums and outputs are 32-bit.  A query row enters the products with 22 bits of its own largest element;
+ * probabilities with 22 bits for SD_FP32 rows and 11 for SD_BF16 ones, and with no less than 2^-35 of the largest V scale that the
+ * rows of its sequence see. */
 typedef struct {
     const int32_t *seq_ids;   /* as above */
     const int32_t *len;
@@ -339,7 +341,7 @@ typedef struct {
     void *out;
     int64_t o_row, o_head;
     float *lse;               /* [rows][n_heads] natural logarithm of the sum of exponentials of the scaled scores, or NULL */
-    float scale;              /* finite */
+    float scale;              /* finite, also times log2(e) */
     int32_t causal, window, sinks;
     void *workspace;          /* sd_kv8_attend_workspace bytes of any contents, 16-byte aligned, this call's alone until its kernels have
                                  run; NULL: one block per (sequence, head) walks the whole context */
