@@ -355,7 +355,7 @@ __device__ __forceinline__ float wave_max(float v)
 }
 
 // How the tiles of all (sequence, cache head, set of rows) units are dealt out.  Units stand in a row, a sequence's next to each other and as
-// long as what any row of the sequence sees and K8_UNIT_COST more (32 x 6 rows over up to 4096 tokens 146 us without, 140 with); block b
+// long as what any row of the sequence sees and K8_UNIT_COST more (32 x 6 rows over up to 4096 tokens 132.8 us without, 130.6 with); block b
 // takes the stretch [b * chunk, (b + 1) * chunk), which may reach over several units and cover parts of the first and the last: every
 // block has the same work, whatever the lengths.  With too little work for that (`cross` = false) units are rounded up to whole
 // stretches instead, and no block has parts of two.
@@ -519,7 +519,7 @@ struct K8Regs {
 // E, a power of two above half the largest V scale so far, takes the scales' range out of the 16-bit probabilities.
 // Bound: memory; per code about 1.2 vector operations to widen it, beside one matrix instruction per 512 codes and 16 rows.
 template <int HD, int MT, int TERMS>
-__global__ __launch_bounds__(256, MT == 1 ? 3 : 2) void kv8_attn_stream_kernel(Kv8View c, Kv8Rows rw, Kv8Attn a, int S, int goal, float *part)
+__global__ __launch_bounds__(256, 2) void kv8_attn_stream_kernel(Kv8View c, Kv8Rows rw, Kv8Attn a, int S, int goal, float *part)
 {
     constexpr int VB = HD / 16, VW = HD / 64, ND = VB, SET = 16 * MT;
     __shared__ __attribute__((aligned(16))) float sO[4][16][HD + 4];
@@ -1215,9 +1215,10 @@ static Kv8Plan kv8_plan(const Kv8View &c, const Kv8Rows &rw, const Kv8Attn &a, i
     if (R <= 64 && (int64_t)a.total_rows * c.kv_heads <= 1 << 24) {
         p.kernel = KV8_STREAM, p.mt = R <= 16 ? 1 : 2, p.max_m = R;
         const int64_t units = (int64_t)rw.n * c.kv_heads * ((R + 16 * p.mt - 1) / (16 * p.mt));
-        // the blocks that 256 compute units hold at once; a unit in about as many parts as there are blocks for it (twice that, and one
-        // more at either end, where lengths differ)
-        p.goal = 256 * (p.mt == 1 ? 3 : 2);
+        // Blocks in multiples of the 256 compute units (32 x 6 rows over up to 4096 tokens of 32 heads of 128, mt = 1: 135 us with one a unit, 122
+        // with two, 130 with three, 142 with six; 4 x 6 x 4 over 65536 of 8, mt = 2: 76 with one, 78 with two); a context in about as many
+        // parts as there are blocks for it (twice that, and one more at either end, where lengths differ)
+        p.goal = p.mt == 1 ? 512 : 256;
         p.splits = tiles <= K8_WHOLE ? 1 : (int)std::min<int64_t>(K8_MAX_SPLITS, 2 + 2 * ((p.goal + units - 1) / units));
         if (ws_bytes >= 0) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(p.splits, ws_bytes / one));
         p.blocks = p.splits > 1 ? p.goal + std::min<int64_t>(units, 2 * p.goal) : units; // (with more units than that kv8_deal makes at most `goal` stretches)
