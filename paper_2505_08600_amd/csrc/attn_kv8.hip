@@ -579,10 +579,13 @@ __global__ __launch_bounds__(256, 2) void kv8_attn_stream_kernel(Kv8View c, Kv8R
         const uint32_t k_lane = qi * HD + 16 * grp, v_lane = 4 * grp * HD + VB * qi; // byte offsets of the lane inside a tile
         // One tile's bytes: they are asked for where the tile before it has used the registers up, K and the scales behind the score
         // products, V behind the output products.
-        K8Regs<HD> r;
+        // One row set of 64 dimensions leaves registers for a second tile in flight (16 x 2 rows in a window of 1024 tokens, 16 heads of 64: 14.5
+        // us with one, 13.1 with two; with 128 dimensions the 122 us of a verify call become 131).
+        constexpr int DEPTH = MT == 1 && HD == 64 ? 2 : 1;
+        K8Regs<HD> r0, r1;
         // (edge: a tile that may reach behind the last token.  Those between the edges are loaded without the question, from a uniform base:
         // 4 x 65536 tokens of 8 heads of 128 for 6 x 32 query rows 85 us with the question everywhere, 79 so.)
-        auto load_k = [&](int t, auto edge) {
+        auto load_k = [&](K8Regs<HD> &r, int t, auto edge) {
             const int t0 = tl.token0(t);
             if (!decltype(edge)::value || t0 + K8_TILE <= tl.hi_max) { // (uniform) a whole tile: one address and constant offsets
                 const int8_t *kt = K + (int64_t)t0 * HD;
@@ -601,7 +604,7 @@ __global__ __launch_bounds__(256, 2) void kv8_attn_stream_kernel(Kv8View c, Kv8R
             const int tok = t0 + (lane & 31);
             r.sc = (lane < 32 ? KS : VS)[min(tok, last_tok)];
         };
-        auto load_v = [&](int t, auto edge) {
+        auto load_v = [&](K8Regs<HD> &r, int t, auto edge) {
             const int t0 = tl.token0(t);
             if (!decltype(edge)::value || t0 + K8_TILE <= tl.hi_max) {
                 const int8_t *vt = V + (int64_t)t0 * HD;
@@ -619,8 +622,12 @@ __global__ __launch_bounds__(256, 2) void kv8_attn_stream_kernel(Kv8View c, Kv8R
         Q16<TERMS> raw[MT][HD / 64];
         load_rows<HD, MT, TERMS>(a, sq, n_rows, kvh, grps, m0, raw);
         if (wave < od.n) { // the first tile is on its way while the queries are looked at
-            load_k(od.tile(wave), std::true_type{});
-            load_v(od.tile(wave), std::true_type{});
+            load_k(r0, od.tile(wave), std::true_type{});
+            load_v(r0, od.tile(wave), std::true_type{});
+            if constexpr (DEPTH == 2) {
+                load_k(r1, od.tile(min(wave + 4, od.n - 1)), std::true_type{});
+                load_v(r1, od.tile(min(wave + 4, od.n - 1)), std::true_type{});
+            }
         }
         // Each row has a scale of its own, whatever the rows beside it hold: a score is its product times the token's scale, a.scale / 2^21
         // (both in sS) and 2^e (q2e, folded into the exponential's argument).  Of a row with a NaN or an infinity everything is NaN.
@@ -636,8 +643,9 @@ __global__ __launch_bounds__(256, 2) void kv8_attn_stream_kernel(Kv8View c, Kv8R
             q2e[mt] = mx >= K8_INF && (seen[mt].hi > seen[mt].lo || seen[mt].n_first) ? NAN : pow2(e);
         }
         // (t_next is asked for whether it is wanted or not: with loads that may be left out, the wait for K would have to be one for V too)
-        auto consume = [&](int t, int t_next, auto masked) {
+        auto consume = [&](K8Regs<HD> &r, int u, auto masked) {
             constexpr bool MASKED = decltype(masked)::value;
+            const int t = od.tile(u), t_next = od.tile(min(u + 4 * DEPTH, od.n - 1));
             const int rel = tl.token0(t) + 4 * grp; // tokens are counted from the lane's first one
             float sc = r.sc;
             if (MASKED) { // V scales of tokens that no row sees are not looked at
@@ -672,7 +680,7 @@ __global__ __launch_bounds__(256, 2) void kv8_attn_stream_kernel(Kv8View c, Kv8R
             const f32x4 va = *(const f32x4 *)&sS[wave][32 + 4 * grp], vb = *(const f32x4 *)&sS[wave][48 + 4 * grp];
             asm volatile("" ::: "memory");
             __builtin_amdgcn_sched_barrier(0);
-            load_k(t_next, masked);
+            load_k(r, t_next, masked);
             __builtin_amdgcn_sched_barrier(0);
             Half8 ph[MT][TERMS];
 #pragma unroll
@@ -738,13 +746,32 @@ __global__ __launch_bounds__(256, 2) void kv8_attn_stream_kernel(Kv8View c, Kv8R
                             o[mt][4 * w + b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[b].v, ph[mt][u].v, o[mt][4 * w + b], 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            load_v(t_next, masked);
+            load_v(r, t_next, masked);
             __builtin_amdgcn_sched_barrier(0);
         };
         if (wave < od.n) {
             int u = wave;
-            for (; u < od.n_edge; u += 4) consume(od.tile(u), od.tile(min(u + 4, od.n - 1)), std::true_type{});
-            for (; u < od.n; u += 4) consume(od.tile(u), od.tile(min(u + 4, od.n - 1)), std::false_type{});
+            if constexpr (DEPTH == 1) {
+                for (; u < od.n_edge; u += 4) consume(r0, u, std::true_type{});
+                for (; u < od.n; u += 4) consume(r0, u, std::false_type{});
+            } else { // the registers take turns
+                auto whole = [&](K8Regs<HD> &x, K8Regs<HD> &y) {
+                    for (; u + 4 < od.n; u += 8) {
+                        consume(x, u, std::false_type{});
+                        consume(y, u + 4, std::false_type{});
+                    }
+                    if (u < od.n) consume(x, u, std::false_type{});
+                };
+                for (; u + 4 < od.n_edge; u += 8) {
+                    consume(r0, u, std::true_type{});
+                    consume(r1, u + 4, std::true_type{});
+                }
+                if (u < od.n_edge) {
+                    consume(r0, u, std::true_type{});
+                    u += 4;
+                    whole(r1, r0);
+                } else whole(r0, r1);
+            }
         }
         // the waves' parts meet: O in true units (E and the shifts undone), weighted by their maxima.  Thread (row, c) of the sum holds
         // VB adjacent dimensions of a row.
