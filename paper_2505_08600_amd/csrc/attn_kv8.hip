@@ -491,7 +491,7 @@ __device__ __forceinline__ float wave_max_dpp(float v)
     return rows4_max(v);
 }
 
-// Codes are read once per call: with the nontemporal hint.
+// Codes are read once per call: with the nontemporal hint (verify, 32 x 6 rows over up to 4096 tokens: 131 us without, 122 with).
 template <typename T>
 __device__ __forceinline__ T read_once(const int8_t *p)
 {
@@ -1242,10 +1242,10 @@ static Kv8Plan kv8_plan(const Kv8View &c, const Kv8Rows &rw, const Kv8Attn &a, i
     if (R <= 64 && (int64_t)a.total_rows * c.kv_heads <= 1 << 24) {
         p.kernel = KV8_STREAM, p.mt = R <= 16 ? 1 : 2, p.max_m = R;
         const int64_t units = (int64_t)rw.n * c.kv_heads * ((R + 16 * p.mt - 1) / (16 * p.mt));
-        // Blocks in multiples of the 256 compute units (32 x 6 rows over up to 4096 tokens of 32 heads of 128, mt = 1: 135 us with one a unit, 122
-        // with two, 130 with three, 142 with six; 4 x 6 x 4 over 65536 of 8, mt = 2: 76 with one, 78 with two); a context in about as many
-        // parts as there are blocks for it (twice that, and one more at either end, where lengths differ)
-        p.goal = p.mt == 1 ? 512 : 256;
+        // Two blocks for each of the 256 compute units (32 x 6 rows over up to 4096 tokens of 32 heads of 128: 135 us with one a unit, 122 with
+        // two, 130 with three, 142 with six; 64 x 50 rows over up to 4000 of 16 of 64: 233 with one, 174 with two); a context in about as
+        // many parts as there are blocks for it (twice that, and one more at either end, where lengths differ)
+        p.goal = 512;
         p.splits = tiles <= K8_WHOLE ? 1 : (int)std::min<int64_t>(K8_MAX_SPLITS, 2 + 2 * ((p.goal + units - 1) / units));
         if (ws_bytes >= 0) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(p.splits, ws_bytes / one));
         p.blocks = p.splits > 1 ? p.goal + std::min<int64_t>(units, 2 * p.goal) : units; // (with more units than that kv8_deal makes at most `goal` stretches)
