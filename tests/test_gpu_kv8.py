@@ -661,6 +661,84 @@ def test_speculation_on_8_bit_caches_follows_plain_decoding():
         assert n > 60 - 10 and a[:n] == s[:n]
 
 
+def test_adapters_on_an_8_bit_cache():
+    """Sequences of one batch with different low-rank adapters: logits against the merged weights in float64 over the keys and values the
+    cache holds."""
+    shape = dg.SHAPES["tiny_target"]
+    w = dg.make_weights(shape, 41)
+    lora, scale, gamma = dg.make_lora(shape, 42, n_adapters=2, rank=4, std_a=0.05, std_b=0.05), 2.0, 3
+    m = api.Model(shape, w, max_rows=64, max_pos=128)
+    m.set_lora(lora, scale)
+    ctx = api.Context([100, 100, 60])
+    ctx.attach_kv8(m)
+    ids = [1, -1, 0]
+    ctx.set_adapters(m, ids)
+    rng = np.random.default_rng(7)
+    seqs = [rng.integers(0, shape.vocab, n).tolist() for n in (70, 33, 20)]
+    ctx.set_tokens(seqs)
+    api.sd_prefill(m, ctx, None, 3, 69)
+    cand = torch.from_numpy(rng.integers(0, shape.vocab, (3, gamma)).astype(np.int32)).cuda()
+    na, nx = torch.zeros(3, dtype=torch.int32).cuda(), torch.zeros(3, dtype=torch.int32).cuda()
+    api.sd_verify(m, ctx, None, 3, gamma, 0.0, cand, None, None, na, nx, commit=False)
+    logits = m.last_logits().cpu().view(3, gamma + 1, -1).double()
+    for b, a in enumerate(ids):
+        wm = dict(w)
+        if a >= 0:
+            for pnm, key in (("q", "wq"), ("k", "wk"), ("v", "wv"), ("o", "wo")):
+                wm[key] = [w[key][l].astype(np.float64) + scale * lora["b_" + pnm][l][a].astype(np.float64) @ lora["a_" + pnm][l][a].astype(np.float64)
+                           for l in range(shape.n_layers)]
+        tokens = seqs[b] + cand[b].tolist()
+        vals = [tuple(torch.from_numpy(x).double() for x in ctx.get_kv(m, l, b, len(tokens))) for l in range(shape.n_layers)]
+        want, made = plain_forward(shape, wm, tokens, lambda l: vals[l])
+        err = (logits[b] - want[-(gamma + 1):]).abs().amax(-1) / want[-(gamma + 1):].abs().amax(-1)
+        assert (err < 1e-4).all(), (b, err)               # (the path's bound on fp32 logits)
+        for x, y in zip(made[0], vals[0]):
+            assert ((x - y).abs() <= x.abs().amax(-1, keepdim=True) * (0.5 / 127 + 1e-4 / 4)).all()
+    ctx.sync(m)
+
+
+@pytest.mark.parametrize("name,dname", [("tiny_target", "tiny_draft"), ("small_target_bf16", "small_draft_bf16")])
+def test_path_on_8_bit_caches_captured_and_replayed(name, dname):
+    """A committing greedy step in a graph, captured at 20 tokens and replayed far past that: the tokens of the same steps launched eagerly."""
+    shape, dshape = dg.SHAPES[name], dg.SHAPES[dname]
+    target, draft = (api.Model(s, dg.make_weights(s, 51), max_rows=64, max_pos=1600) for s in (shape, dshape))
+    prompt, gamma, steps = [np.random.default_rng(8).integers(0, shape.vocab, n).tolist() for n in (20, 1400)], 3, 24
+    cand = torch.zeros(2, gamma, dtype=torch.int32).cuda()
+    na, nx = torch.zeros(2, dtype=torch.int32).cuda(), torch.zeros(2, dtype=torch.int32).cuda()
+
+    def new_ctx():
+        c = api.Context([160, 1560])
+        c.attach_kv8(target)
+        c.attach_kv8(draft, 16, 2)
+        c.set_tokens(prompt)
+        api.sd_prefill(target, c, None, 2, 1399)
+        api.sd_prefill(draft, c, None, 2, 1399)
+        return c
+
+    def step(c):
+        api.sd_draft(draft, c, None, 2, gamma, 0.0, None, cand, None)
+        api.sd_verify(target, c, None, 2, gamma, 0.0, cand, None, None, na, nx, commit=True)
+
+    eager = new_ctx()
+    for _ in range(steps):
+        step(eager)
+    eager.sync()
+    want = [list(eager.get_tokens(b)) for b in range(2)]
+    ctx = new_ctx()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            step(ctx)
+    torch.cuda.synchronize()
+    for k in range(steps):
+        graph.replay()
+        torch.cuda.synchronize()
+    ctx.sync()
+    assert [list(ctx.get_tokens(b)) for b in range(2)] == want and len(want[0]) >= 20 + steps
+
+
 def test_attach_and_cache_rows():
     shape = dg.SHAPES["small_target_bf16"]
     m = api.Model(shape, dg.make_weights(shape, 3), max_rows=32, max_pos=128)
