@@ -168,28 +168,27 @@ __device__ __forceinline__ int64_t row_place(const Kv8View &c, const Kv8Rows &rw
     return c.off[b] + t;
 }
 
-// Both kernels: a block serves RB adjacent rows (RB > 1: and memory with the nontemporal hint).  Its first threads find the rows' places;
+// Both kernels: a block serves 2^row_bits adjacent rows.  Its first threads find the rows' places;
 // pieces of 8 elements are then dealt out with a vector's lanes innermost, then the rows, then the vectors (K and V of each head), so
 // that the codes of adjacent tokens are touched together, and four at a time per thread, so that their loads are in flight together.
-template <int RB>
+#define KV8_MAX_ROWS 32 // of a block
 struct Kv8Piece {
     int l, row, w; // lane of the vector, row of the block, vector (2 * head + (0: K, 1: V))
 };
-template <int RB>
-__device__ __forceinline__ Kv8Piece<RB> kv8_piece(int u, int lane_bits)
+__device__ __forceinline__ Kv8Piece kv8_piece(int u, int lane_bits, int row_bits)
 {
-    return Kv8Piece<RB>{u & ((1 << lane_bits) - 1), (u >> lane_bits) % RB, (u >> lane_bits) / RB};
+    return Kv8Piece{u & ((1 << lane_bits) - 1), (u >> lane_bits) & ((1 << row_bits) - 1), u >> (lane_bits + row_bits)};
 }
 
-template <typename T, bool WIDE, int RB>
-__global__ __launch_bounds__(256) void kv8_append_kernel(Kv8View c, Kv8Rows rw, int n_rows, int lane_bits, const T *__restrict__ k, int64_t k_row,
+template <typename T, bool WIDE, bool NT>
+__global__ __launch_bounds__(256) void kv8_append_kernel(Kv8View c, Kv8Rows rw, int n_rows, int lane_bits, int row_bits, const T *__restrict__ k, int64_t k_row,
                                                          int64_t k_head, const T *__restrict__ v, int64_t v_row, int64_t v_head)
 {
-    __shared__ int64_t s_at[RB];
-    const int r0 = blockIdx.x * RB;
-    if (threadIdx.x < RB) s_at[threadIdx.x] = r0 + (int)threadIdx.x < n_rows ? row_place(c, rw, r0 + threadIdx.x, blockIdx.y == 0) : -1;
+    __shared__ int64_t s_at[KV8_MAX_ROWS];
+    const int r0 = blockIdx.x << row_bits;
+    if (threadIdx.x < 1u << row_bits) s_at[threadIdx.x] = r0 + (int)threadIdx.x < n_rows ? row_place(c, rw, r0 + threadIdx.x, blockIdx.y == 0) : -1;
     __syncthreads();
-    const int n = (2 * c.kv_heads * RB) << lane_bits;
+    const int n = 2 * c.kv_heads << (lane_bits + row_bits);
     for (int u0 = blockIdx.y * 1024; u0 < n; u0 += gridDim.y * 1024) { // (the same count for every lane: shuffles)
         float x[4][8];
 #pragma unroll
@@ -197,16 +196,16 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8View c, Kv8Rows rw, 
 #pragma unroll
             for (int e = 0; e < 8; e++) x[q][e] = 0.f;
             const int u = u0 + 256 * q + threadIdx.x;
-            const Kv8Piece<RB> p = kv8_piece<RB>(u, lane_bits);
+            const Kv8Piece p = kv8_piece(u, lane_bits, row_bits);
             if (u >= n || p.l * 8 >= c.hd || s_at[p.row] < 0) continue;
             const int64_t r = r0 + p.row;
             const int h = p.w >> 1;
-            load8<T, WIDE, (RB > 1)>(p.w & 1 ? v + r * v_row + h * v_head : k + r * k_row + h * k_head, p.l, c.hd, x[q]);
+            load8<T, WIDE, NT>(p.w & 1 ? v + r * v_row + h * v_head : k + r * k_row + h * k_head, p.l, c.hd, x[q]);
         }
 #pragma unroll
         for (int q = 0; q < 4; q++) {
             const int u = u0 + 256 * q + threadIdx.x;
-            const Kv8Piece<RB> p = kv8_piece<RB>(u, lane_bits);
+            const Kv8Piece p = kv8_piece(u, lane_bits, row_bits);
             const float s = kv8_scale(amax_lanes(amax_bits8(x[q]), lane_bits)), inv = 1.0f / s;
             if (u >= n || p.l * 8 >= c.hd || s_at[p.row] < 0) continue;
             const int64_t row = (int64_t)(p.w >> 1) * c.tokens + s_at[p.row];
@@ -217,15 +216,15 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8View c, Kv8Rows rw, 
     }
 }
 
-template <typename T, bool WIDE, int RB>
-__global__ __launch_bounds__(256) void kv8_read_kernel(Kv8View c, Kv8Rows rw, int n_rows, int lane_bits, T *__restrict__ k, int64_t k_row,
+template <typename T, bool WIDE, bool NT>
+__global__ __launch_bounds__(256) void kv8_read_kernel(Kv8View c, Kv8Rows rw, int n_rows, int lane_bits, int row_bits, T *__restrict__ k, int64_t k_row,
                                                        int64_t k_head, T *__restrict__ v, int64_t v_row, int64_t v_head)
 {
-    __shared__ int64_t s_at[RB];
-    const int r0 = blockIdx.x * RB;
-    if (threadIdx.x < RB) s_at[threadIdx.x] = r0 + (int)threadIdx.x < n_rows ? row_place(c, rw, r0 + threadIdx.x, blockIdx.y == 0) : -1;
+    __shared__ int64_t s_at[KV8_MAX_ROWS];
+    const int r0 = blockIdx.x << row_bits;
+    if (threadIdx.x < 1u << row_bits) s_at[threadIdx.x] = r0 + (int)threadIdx.x < n_rows ? row_place(c, rw, r0 + threadIdx.x, blockIdx.y == 0) : -1;
     __syncthreads();
-    const int n = (2 * c.kv_heads * RB) << lane_bits;
+    const int n = 2 * c.kv_heads << (lane_bits + row_bits);
     for (int u0 = blockIdx.y * 1024; u0 < n; u0 += gridDim.y * 1024) {
         uint2 w[4];
         float s[4];
@@ -233,23 +232,23 @@ __global__ __launch_bounds__(256) void kv8_read_kernel(Kv8View c, Kv8Rows rw, in
 #pragma unroll
         for (int q = 0; q < 4; q++) {
             const int u = u0 + 256 * q + threadIdx.x;
-            const Kv8Piece<RB> p = kv8_piece<RB>(u, lane_bits);
+            const Kv8Piece p = kv8_piece(u, lane_bits, row_bits);
             live[q] = u < n && p.l * 8 < c.hd && s_at[p.row] >= 0 && (p.w & 1 ? v : k);
             if (!live[q]) continue;
             const int64_t row = (int64_t)(p.w >> 1) * c.tokens + s_at[p.row];
-            w[q] = load_codes<T, (RB > 1)>((p.w & 1 ? c.v : c.k) + row * c.hd, p.l, c.hd);
+            w[q] = load_codes<T, NT>((p.w & 1 ? c.v : c.k) + row * c.hd, p.l, c.hd);
             s[q] = (p.w & 1 ? c.vs : c.ks)[row];
         }
 #pragma unroll
         for (int q = 0; q < 4; q++) {
             if (!live[q]) continue;
-            const Kv8Piece<RB> p = kv8_piece<RB>(u0 + 256 * q + threadIdx.x, lane_bits);
+            const Kv8Piece p = kv8_piece(u0 + 256 * q + threadIdx.x, lane_bits, row_bits);
             const int64_t r = r0 + p.row;
             const int h = p.w >> 1;
             float x[8];
             dequantise4(w[q].x, s[q], x);
             dequantise4(w[q].y, s[q], x + 4);
-            store8<T, WIDE, (RB > 1)>(p.w & 1 ? v + r * v_row + h * v_head : k + r * k_row + h * k_head, p.l, c.hd, x);
+            store8<T, WIDE, NT>(p.w & 1 ? v + r * v_row + h * v_head : k + r * k_row + h * k_head, p.l, c.hd, x);
         }
     }
 }
@@ -265,36 +264,42 @@ static bool wide_rows(int esz, const void *p, int64_t row, int64_t head)
 {
     return ((uintptr_t)p % 16) == 0 && row * esz % 16 == 0 && head * esz % 16 == 0;
 }
-// Few bytes: a row per block, and its vectors spread over blocks too, so that the chip fills.  Many (2^23 elements of K: more than stays in
-// a cache beside what else a step touches): eight adjacent rows per block, whose codes lie together, and the nontemporal hint.  Rows of
-// 8 heads of 128, bf16: 2048 of them appended 7.3 us with one row per block, 7.9 with eight; 51200 appended 100 with one, 75 with four,
-// 71 with eight, 78 with 32, read back 90, 69, 68, 71 (fp32: 105, 99, 101, 112 and 127, 108, 115, 122).
-#define KV8_ROWS 8
-static int kv8_rows_per_block(int n_rows, const Kv8View &c) { return (int64_t)n_rows * c.kv_heads * c.hd >= 1 << 23 ? KV8_ROWS : 1; }
-static dim3 vector_grid(int n_rows, int rb, int kv_heads, int lane_bits)
+// Rows of a block, as a power of two: enough for two pieces a thread as long as 512 blocks are left (35000 rows of 2 heads of 64, bf16, in and
+// out: 43 and 38 us with a row per block, 12 and 10 so; 2048 rows of 8 of 128 7.1 and 5.5 either way).  `many` (2^23 elements of K: more
+// than stays in a cache beside what else a step touches): eight at least, whose codes lie together, and the nontemporal hint: 51200
+// rows of 8 heads of 128, bf16, one row per block and eight: 100 and 71 us in, 90 and 68 out; 32 rows 78 and 71.
+static int kv8_row_bits(int n_rows, int pieces, bool many)
 {
-    const int gx = (n_rows + rb - 1) / rb, turns = ((2 * kv_heads * rb << lane_bits) + 1023) / 1024;
+    int b = many ? 3 : 0;
+    while (1 << b < KV8_MAX_ROWS && (int64_t)pieces << b < 512 && n_rows >> (b + 1) >= 512) b++;
+    return b;
+}
+static dim3 vector_grid(int n_rows, int row_bits, int pieces)
+{
+    const int gx = (n_rows + (1 << row_bits) - 1) >> row_bits, turns = (int)((((int64_t)pieces << row_bits) + 1023) / 1024);
     return dim3(gx, std::max(1, std::min(turns, 2048 / gx)));
 }
 
 #define KV8_MOVE(KERNEL, CV)                                                                                                                   \
-    const int esz = dtype == SD_BF16 ? 2 : 4, bits = vector_lane_bits(c.hd), rb = kv8_rows_per_block(n_rows, c);                               \
+    const int esz = dtype == SD_BF16 ? 2 : 4, bits = vector_lane_bits(c.hd), pieces = 2 * c.kv_heads << bits;                                  \
     const bool wide = wide_rows(esz, k, k_row, k_head) && wide_rows(esz, v, v_row, v_head); /* (a null pointer counts as aligned) */            \
-    const dim3 grid = vector_grid(n_rows, rb, c.kv_heads, bits);                                                                               \
+    const bool many = (int64_t)n_rows * c.kv_heads * c.hd >= 1 << 23;                                                                          \
+    const int row_bits = kv8_row_bits(n_rows, pieces, many);                                                                                   \
+    const dim3 grid = vector_grid(n_rows, row_bits, pieces);                                                                                   \
     if (dtype == SD_BF16) {                                                                                                                    \
-        if (wide && rb > 1) KV8_GO(KERNEL, CV bf16_t, bf16_t, true, KV8_ROWS);                                                                 \
-        else if (wide) KV8_GO(KERNEL, CV bf16_t, bf16_t, true, 1);                                                                             \
-        else if (rb > 1) KV8_GO(KERNEL, CV bf16_t, bf16_t, false, KV8_ROWS);                                                                   \
-        else KV8_GO(KERNEL, CV bf16_t, bf16_t, false, 1);                                                                                      \
+        if (wide && many) KV8_GO(KERNEL, CV bf16_t, bf16_t, true, true);                                                                       \
+        else if (wide) KV8_GO(KERNEL, CV bf16_t, bf16_t, true, false);                                                                         \
+        else if (many) KV8_GO(KERNEL, CV bf16_t, bf16_t, false, true);                                                                         \
+        else KV8_GO(KERNEL, CV bf16_t, bf16_t, false, false);                                                                                  \
     } else {                                                                                                                                   \
-        if (wide && rb > 1) KV8_GO(KERNEL, CV float, float, true, KV8_ROWS);                                                                   \
-        else if (wide) KV8_GO(KERNEL, CV float, float, true, 1);                                                                               \
-        else if (rb > 1) KV8_GO(KERNEL, CV float, float, false, KV8_ROWS);                                                                     \
-        else KV8_GO(KERNEL, CV float, float, false, 1);                                                                                        \
+        if (wide && many) KV8_GO(KERNEL, CV float, float, true, true);                                                                         \
+        else if (wide) KV8_GO(KERNEL, CV float, float, true, false);                                                                           \
+        else if (many) KV8_GO(KERNEL, CV float, float, false, true);                                                                           \
+        else KV8_GO(KERNEL, CV float, float, false, false);                                                                                    \
     }                                                                                                                                          \
     return hipGetLastError();
-#define KV8_GO(KERNEL, P, T, W, RB) \
-    hipLaunchKernelGGL((KERNEL<T, W, RB>), grid, dim3(256), 0, s, c, rw, n_rows, bits, (P *)k, k_row, k_head, (P *)v, v_row, v_head)
+#define KV8_GO(KERNEL, P, T, W, NT) \
+    hipLaunchKernelGGL((KERNEL<T, W, NT>), grid, dim3(256), 0, s, c, rw, n_rows, bits, row_bits, (P *)k, k_row, k_head, (P *)v, v_row, v_head)
 
 hipError_t launch_kv8_append(hipStream_t s, const Kv8View &c, const Kv8Rows &rw, int n_rows, int dtype, const void *k, int64_t k_row,
                              int64_t k_head, const void *v, int64_t v_row, int64_t v_head)
