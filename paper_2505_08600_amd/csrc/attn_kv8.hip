@@ -151,7 +151,7 @@ typedef __attribute__((ext_vector_type(4))) float f32x4;
 #define K8_WHOLE 40
 #define K8_MIN_TILES 8
 #define K8_MIN_SPLIT 16  // many rows: tiles of a split at least
-#define K8_MAX_SPLITS 64 // splits of a context at most
+#define K8_MAX_SPLITS 64 // splits of a context at most (of 4096 tiles or more, few rows: twice that)
 #define K8_P_SHIFT 14 // probabilities enter as p * (vs / E) * 2^14 < 2^15
 
 union Half8 {
@@ -1241,7 +1241,10 @@ static Kv8Plan kv8_plan(const Kv8View &c, const Kv8Rows &rw, const Kv8Attn &a, i
         // two, 130 with three, 142 with six; 64 x 50 rows over up to 4000 of 16 of 64: 233 with one, 174 with two); a context in about as
         // many parts as there are blocks for it (twice that, and one more at either end, where lengths differ)
         p.goal = 512;
-        p.splits = tiles <= K8_WHOLE ? 1 : (int)std::min<int64_t>(K8_MAX_SPLITS, 2 + 2 * ((p.goal + units - 1) / units));
+        // (but for few units of long contexts: one in a million tokens and 2 heads of 128 141 us with 64 parts, 96 with 128; in 32768 tokens and 4
+        // heads 25 and 29, the join being longer)
+        const int64_t most = tiles >= 4096 ? 2 * K8_MAX_SPLITS : K8_MAX_SPLITS;
+        p.splits = tiles <= K8_WHOLE ? 1 : (int)std::min<int64_t>(most, 2 + 2 * ((p.goal + units - 1) / units));
         if (ws_bytes >= 0) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(p.splits, ws_bytes / one));
         p.blocks = p.splits > 1 ? p.goal + std::min<int64_t>(units, 2 * p.goal) : units; // (with more units than that kv8_deal makes at most `goal` stretches)
     } else {

@@ -445,6 +445,15 @@ def test_one_long_context_among_very_many(workspace):
     close((out[some], lse[some]), tuple(t[some] for t in want))
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_a_context_in_the_most_parts(dtype):
+    """A token over 200000 others, one cache head: 4096 tiles and more."""
+    n = 200_000
+    ref = kv8ref.Cache([n + 1], 1, 64).fill(12)
+    q = torch.randn(1, 2, 64, generator=torch.Generator().manual_seed(2)).to(dtype)
+    close(run_attend(ref.to_gpu(), q, [n], [1], 0.125, ragged=False), kv8ref.attend(ref, q, [(0, n, 0, 1)], 0.125))
+
+
 @pytest.mark.parametrize("rows,dim", [(3, 128), (5, 64), (100, 128)])
 def test_workspace_contents_do_not_matter(rows, dim):
     lens = [4000, 30, 1500]
