@@ -425,9 +425,9 @@ __device__ __forceinline__ Kv8Deal kv8_deal(const Kv8View &c, const Kv8Rows &rw,
     int T_max = max(1, d.mine.T);
     for (int j = lane + 64; j - lane < rw.n; j += 64) T_max = max(T_max, kv8_units<SET>(c, rw, a, j).T);
     T_max = wave_most(T_max);
-    // at most `units` of them (two for a row and cache head; 2^25: kv8_plan), so that 2^29 positions hold all and the longest is no longer
-    // than 2^18
-    const uint64_t units = (uint64_t)(unsigned)a.total_rows * (unsigned)c.kv_heads * 2, most = units * (unsigned)(T_max + K8_UNIT_COST) >> 29 | (unsigned)T_max >> 18;
+    // at most `units` of them (two for a row and cache head; 2^25: kv8_plan), so that 2^28 positions hold all (a block's next stretch may lie
+    // four times as far) and the longest is no longer than 2^18
+    const uint64_t units = (uint64_t)(unsigned)a.total_rows * (unsigned)c.kv_heads * 2, most = units * (unsigned)(T_max + K8_UNIT_COST) >> 28 | (unsigned)T_max >> 18;
     d.grain = most ? 64 - __builtin_clzll(most) : 0;
     T_max = (T_max + (1 << d.grain) - 1) >> d.grain;
     d.cross = true;
